@@ -16,6 +16,10 @@
  * byte read once); nsd_copy_plan moves KV between a pinned host arena and a
  * device bank (the host-side source of the preparation).
  *
+ * A request's prompt is processed before its rounds: nsd_plan_blocks (blocks
+ * and slots of a step's tokens), then per layer nsd_rope_append and
+ * nsd_chunk_attention; nsd_trim_blocks gives blocks back.
+ *
  * Conventions shared by every call
  * --------------------------------
  * - Pointers named as device pointers must address memory the GPU of
@@ -507,6 +511,152 @@ nsd_status nsd_sample_steps(const float* probs, int64_t row_stride, const float*
                             int32_t n, int32_t steps, int32_t vocab, int32_t* out_tokens,
                             int32_t out_stride, void* workspace, size_t workspace_bytes,
                             void* stream);
+
+/*
+ * Blocks and cache slots of a step's new tokens, and the blocks that finished
+ * or shortened requests give back: block tables, slot maps and the free list
+ * kept on the device, so a step's bookkeeping needs no host round trip.
+ *
+ * Passage: Section 3 (paged KV blocks and a block map per request; the cache is
+ * append-dominant); Appendix F.2 (a request joins where its blocks fit).
+ *
+ * Request r holds owned[r] blocks (block_table[r][0 .. owned[r])) and
+ * seq_lens[r] cached tokens; its new tokens are rows q_indptr[r] ..
+ * q_indptr[r+1] - 1 of the step, n_r of them.  It needs
+ * max(0, ceil((seq_lens[r] + n_r) / 16) - owned[r]) more blocks.  Requests are
+ * served in order: r is granted if it needs none, or if its needs and those of
+ * all requests before it (granted or not) are at most free_count[0].  A request
+ * whose tokens do not fit its table row (ceil(..) > max_blocks_per_seq) is not
+ * granted and counts no need.  The free list is a stack, free_blocks[0 ..
+ * free_count[0]), whose last entry is taken first.
+ *
+ * nsd_plan_blocks: a granted request's new ids go to its table row's entries
+ * owned[r].. (no other entry is written); granted[r] = 1,
+ * new_owned[r] = owned[r] + its needs, new_lens[r] = seq_lens[r] + n_r, and the
+ * slot of its token j, at position t = seq_lens[r] + j, is
+ * slots[q_indptr[r] + j] = block_table[r][t / 16] * 16 + t % 16 (-1 where the
+ * id is not in [0, 2^27)).  A request not granted keeps its counters, with
+ * granted[r] = 0 and slots of -1.  new_free_count[0] = what is left.
+ *
+ * nsd_trim_blocks: request r keeps ceil(keep_lens[r] / 16) blocks (at most
+ * owned[r]); the ids of its other blocks are pushed onto the free list,
+ * requests and table entries in ascending order, at
+ * free_blocks[free_count[0]]...  Table entries past new_owned[r] keep their
+ * ids and no longer belong to the request.  Ids beyond free_capacity are
+ * dropped.
+ *
+ * All arrays device int32: block_table [bs][max_blocks_per_seq]; owned,
+ * seq_lens, keep_lens, granted, new_* [bs]; q_indptr [bs+1]; slots [total_q];
+ * free_blocks [free_capacity]; free_count, new_free_count [1].  new_owned,
+ * new_lens and new_free_count may be owned, seq_lens and free_count themselves
+ * (updated in place); no other two arrays overlap.  Negative lengths and counts
+ * count as 0, owned is clamped to the row, q_indptr to [0, total_q].
+ * 0 <= bs <= 8192; free_capacity <= 2^27.  bs == 0 copies the count.
+ */
+nsd_status nsd_plan_blocks(int32_t* block_table, int32_t max_blocks_per_seq,
+                           const int32_t* owned, const int32_t* seq_lens,
+                           const int32_t* q_indptr, int32_t bs, int32_t total_q,
+                           const int32_t* free_blocks, int32_t free_capacity,
+                           const int32_t* free_count, int32_t* new_owned, int32_t* new_lens,
+                           int32_t* new_free_count, int32_t* granted, int32_t* slots,
+                           void* stream);
+nsd_status nsd_trim_blocks(const int32_t* block_table, int32_t max_blocks_per_seq,
+                           const int32_t* owned, const int32_t* keep_lens, int32_t bs,
+                           int32_t* free_blocks, int32_t free_capacity,
+                           const int32_t* free_count, int32_t* new_owned,
+                           int32_t* new_free_count, void* stream);
+
+/*
+ * Rotary positions of a step's query and key rows, and its K/V rows into their
+ * cache slots, for one layer.
+ *
+ * Passage: Section 3 (an iteration adds the K/V of the tokens it processed);
+ * Section 6 setup (the served models are rotary transformers).
+ *
+ * Pair i < rot_dim / 2 of a head is its dimensions (i, i + rot_dim / 2), or
+ * (2i, 2i + 1) with interleaved != 0; it belongs to the axis a whose section
+ * holds i (sections[0] pairs for axis 0, then sections[1], ...) and turns by
+ * angle = positions[a][row] * inv_freq[i] (the product and its reduction to a
+ * turn in fp64): (x, y) -> (x cos - y sin, x sin + y cos), computed in fp32 and
+ * rounded to bf16.  Dimensions from rot_dim on pass unchanged.
+ *     q_out[row][h] = turned q[row][h]
+ *     K plane, slot slots[row], head g <- turned k_new[row][g]
+ *     V plane, slot slots[row], head g <- v_new[row][g]
+ * A row whose slot is outside [0, 16 * num_blocks) (such as -1) is turned into
+ * q_out but not cached.  No other slot is written, whatever order the slots
+ * come in; of rows naming one slot any one's values stay, element by element.
+ *
+ * q, k_new, v_new : device bf16 rows of [num_q_heads][head_dim] and
+ *     [num_kv_heads][head_dim], the rows q_stride, k_stride and v_stride
+ *     elements apart (multiples of 8: views of a fused projection's output);
+ *     bases 16-byte aligned.  q_out : device bf16 [total_q][num_q_heads][head_dim],
+ *     which may be q itself where q's rows are dense.
+ * positions : device int32 [n_axes][total_q], any values; inv_freq : device
+ *     fp32 [rot_dim / 2]; sections : host int32 [n_axes] with sum rot_dim / 2
+ *     (NULL for one axis); 1 <= n_axes <= 4.
+ * rot_dim : a multiple of 16 in [0, head_dim] (0: the rows are only cached).
+ * slots : device int32 [total_q], as nsd_plan_blocks gives them.
+ * k_pool, v_pool : this layer's planes; num_blocks <= 2^27.
+ * head_dim in {64, 128}; block_size == 16.  total_q == 0 is a no-op.
+ */
+nsd_status nsd_rope_append(void* k_pool, void* v_pool, int64_t num_blocks, const void* q,
+                           int64_t q_stride, const void* k_new, int64_t k_stride,
+                           const void* v_new, int64_t v_stride, const int32_t* positions,
+                           const float* inv_freq, const int32_t* sections, int32_t n_axes,
+                           int32_t rot_dim, int32_t interleaved, const int32_t* slots,
+                           int32_t total_q, int32_t num_q_heads, int32_t num_kv_heads,
+                           int32_t block_size, int32_t head_dim, void* q_out, void* stream);
+
+/*
+ * Attention of each request's new tokens over its paged cache, for one layer:
+ * a prompt's chunk of any length, or single tokens, in one batch.
+ *
+ * Passage: Section 3 (a request's prefill precedes its speculative rounds; the
+ * cache already holds the chunk's own states); Section 1.
+ *
+ * Queries, cache, block_table, seq_lens and q_indptr as in
+ * nsd_verify_attention, without its limit on the rows: query j of request r
+ * sits at position p = L_r - n_q + j.  It sees token t < L_r iff
+ *     t < prefix_lens[r],  or  first_keys[q_indptr[r] + j] <= t <= p,
+ * and t's block id is valid.  With x = scale <q, k_t>,
+ *     y_t = softcap * tanh(x / softcap) (x itself where softcap is 0)
+ *           - slopes[h] * |p - t| (where slopes are given),
+ *     out = softmax_t(y_t) . v_t
+ * in fp32 from bf16 inputs (the weights enter the second product as bf16; rows
+ * split over workgroups are joined in fp32); out is rounded to bf16.  A row
+ * that sees no token, or only scores of -infinity, is 0.  Tokens that a row does
+ * not see do not affect it, whatever their K and V hold; an infinity or NaN in
+ * V of a token that it sees makes the row's dimension infinite or NaN.
+ *
+ * first_keys : device int32 [total_q] or NULL (0): the first key of a sliding
+ *     window, or of the query's document among those packed into a request.
+ * prefix_lens : device int32 [bs] or NULL (0): tokens every query of the
+ *     request sees, also those after it (clamped to [0, L_r]).
+ * slopes : device fp32 [num_q_heads], finite, or NULL.  softcap >= 0, finite.
+ * seq_lens : L_r beyond max_seq_len or the table's row are clamped.  A request
+ *     may have no new token; one with L_r < n_q has rows that see nothing
+ *     before position 0.
+ * total_q : rows of q and out; q_indptr entries are clamped into [0, total_q].
+ *     total_q * num_q_heads <= 2^31 - 1.  max_q_per_seq >= 1 bounds n_q.
+ * head_dim in {64, 128}; any num_q_heads / num_kv_heads; block_size == 16;
+ * q, out and the caches 16-byte aligned; out may not alias an input.
+ * workspace : device, 16-byte aligned, at least
+ *     nsd_chunk_attention_workspace_size(...) bytes (may be 0), any contents;
+ *     calls that overlap in time need separate ones.
+ * 0 <= bs <= 8192; bs == 0 or total_q == 0 is a no-op.
+ */
+size_t     nsd_chunk_attention_workspace_size(int32_t bs, int32_t total_q, int32_t num_q_heads,
+                                              int32_t num_kv_heads, int32_t head_dim,
+                                              int32_t max_q_per_seq, int32_t max_seq_len);
+nsd_status nsd_chunk_attention(const void* q, const void* k_cache, const void* v_cache,
+                               int64_t num_blocks, const int32_t* block_table,
+                               int32_t max_blocks_per_seq, const int32_t* seq_lens,
+                               const int32_t* q_indptr, int32_t bs, int32_t total_q,
+                               int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                               int32_t block_size, int32_t max_q_per_seq, int32_t max_seq_len,
+                               float scale, float softcap, const float* slopes,
+                               const int32_t* first_keys, const int32_t* prefix_lens, void* out,
+                               void* workspace, size_t workspace_size, void* stream);
 
 /*
  * Host validation of a round's metadata: host copies of the arrays the

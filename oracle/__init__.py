@@ -19,6 +19,8 @@ Plain, slow, fp64 numpy restatements of what the round computes:
 * ``schedule``  -- worker-triggered batch reconstruction (Algorithm 1,
                    Eqs. 4-8) and the profiling-driven discrete-event
                    simulator with ideal migration (Appendix H).
+* ``prompt``    -- blocks and slots of a step's new tokens, rotary positions,
+                   attention of a prompt's chunk (Section 3).
 
 Only the test suite, ``__graft_entry__.smoke()`` and the ``cpu_baseline`` leg of
 ``bench.py`` may import this package.  It shares no code with the HIP library
@@ -29,6 +31,6 @@ Every function is pinned by ``tests/test_oracle_*.py`` against a library
 routine, closed forms, invariants or a sampling theorem; none is "parity
 unpinned".
 """
-from . import gather, attention, accept, commit, draft, schedule
+from . import gather, attention, accept, commit, draft, schedule, prompt
 
-__all__ = ["gather", "attention", "accept", "commit", "draft", "schedule"]
+__all__ = ["gather", "attention", "accept", "commit", "draft", "schedule", "prompt"]

@@ -69,6 +69,14 @@ _SIGS = {
     "nsd_spec_accept_static_max_bytes": (_SZ, []),
     "nsd_set_attention_waves": (_I32, [_I32]),
     "nsd_attention_waves": (_I32, []),
+    "nsd_plan_blocks": (_I32, [_P, _I32, _P, _P, _P, _I32, _I32, _P, _I32, _P, _P, _P, _P, _P, _P,
+                               _P]),
+    "nsd_trim_blocks": (_I32, [_P, _I32, _P, _P, _I32, _P, _I32, _P, _P, _P, _P]),
+    "nsd_rope_append": (_I32, [_P, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _P, _P, _I32, _I32,
+                               _I32, _P, _I32, _I32, _I32, _I32, _I32, _P, _P]),
+    "nsd_chunk_attention_workspace_size": (_SZ, [_I32] * 7),
+    "nsd_chunk_attention": (_I32, [_P, _P, _P, _I64, _P, _I32, _P, _P, _I32, _I32, _I32, _I32, _I32,
+                                   _I32, _I32, _I32, _F32, _F32, _P, _P, _P, _P, _P, _SZ, _P]),
     "nsd_check_plan": (_I32, [_P, _P, _I32, _P, _P, _I32, _I64, _I64, _I32, _I32, _I64]),
     "nsd_check_pairs": (_I32, [_P, _P, _I64, _I64, _I64]),
 }
@@ -94,7 +102,9 @@ BINDING_PATH = os.path.join(HERE, "_nsd_torch.so")
 _BOUND = ("nsd_kv_gather", "nsd_verify_attention", "nsd_gather_verify_attention",
           "nsd_verify_attention_workspace_size", "nsd_spec_accept",
           "nsd_spec_accept_workspace_size", "nsd_sample", "nsd_kv_append", "nsd_commit_lengths",
-          "nsd_kv_append_layers", "nsd_spec_accept_commit", "nsd_sample_steps")
+          "nsd_kv_append_layers", "nsd_spec_accept_commit", "nsd_sample_steps", "nsd_plan_blocks",
+          "nsd_trim_blocks", "nsd_rope_append", "nsd_chunk_attention",
+          "nsd_chunk_attention_workspace_size")
 _native_module = None
 
 
@@ -591,7 +601,237 @@ def kv_writeback(k_pool, v_pool, host_k, host_v, src_ids, dst_ids):
         BLOCK_SIZE, d, _stream(k_pool)))
 
 
+def _same_device(t, **others):
+    for name, o in others.items():
+        if o is not None and o.device != t.device:
+            raise ValueError(f"{name} must be on {t.device}")
+
+
+def _i32s(n, name, t, out=None):
+    """A checked int32 GPU tensor of n entries (a new one beside `out` where t is None)."""
+    if t is None and out is not None:
+        return torch.empty(n, dtype=torch.int32, device=out.device)
+    _dev(t, torch.int32, name)
+    if t.numel() != n:
+        raise ValueError(f"{name} must have {n} entries")
+    return t
+
+
+def plan_blocks(block_table, owned, seq_lens, q_indptr, free_blocks, free_count, total_q,
+                new_owned=None, new_lens=None, new_free_count=None, granted=None, slots=None):
+    """Blocks and cache slots of a step's new tokens; returns (new_owned, new_lens,
+    new_free_count, granted, slots), int32.
+
+    block_table [bs][max_blocks] (the new ids are written into it); owned and seq_lens
+    [bs]: the blocks and cached tokens of each request; q_indptr [bs+1]: offsets of its
+    new tokens, total_q = q_indptr[bs] of them (a host integer); free_blocks: the free
+    list, a stack of free_count[0] ids.  Requests that do not fit are not granted
+    (granted 0, slots -1, counters unchanged).  new_owned, new_lens and new_free_count
+    may be owned, seq_lens and free_count themselves, to update a batch in place.
+    """
+    r = (_native_module or _native()).plan_blocks(
+        block_table, owned, seq_lens, q_indptr, free_blocks, free_count, total_q, new_owned,
+        new_lens, new_free_count, granted, slots)
+    if r is not None:
+        _raised(r)
+        return tuple(r)
+    _dev(block_table, torch.int32, "block_table")
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [bs][max_blocks]")
+    bs = block_table.shape[0]
+    owned, seq_lens = _i32s(bs, "owned", owned), _i32s(bs, "seq_lens", seq_lens)
+    q_indptr = _i32s(bs + 1, "q_indptr", q_indptr)
+    _dev(free_blocks, torch.int32, "free_blocks")
+    free_count = _i32s(1, "free_count", free_count)
+    new_owned = _i32s(bs, "new_owned", new_owned, owned)
+    new_lens = _i32s(bs, "new_lens", new_lens, owned)
+    new_free_count = _i32s(1, "new_free_count", new_free_count, owned)
+    granted = _i32s(bs, "granted", granted, owned)
+    if total_q < 0:
+        raise ValueError("total_q must not be negative")
+    slots = _i32s(total_q, "slots", slots, owned)
+    _same_device(block_table, owned=owned, seq_lens=seq_lens, q_indptr=q_indptr,
+                 free_blocks=free_blocks, free_count=free_count, new_owned=new_owned,
+                 new_lens=new_lens, new_free_count=new_free_count, granted=granted, slots=slots)
+    with torch.cuda.device(block_table.device):
+        _check("plan_blocks", lib().nsd_plan_blocks(
+            _ptr(block_table), block_table.shape[1], _ptr(owned), _ptr(seq_lens), _ptr(q_indptr),
+            bs, total_q, _ptr(free_blocks), free_blocks.numel(), _ptr(free_count),
+            _ptr(new_owned), _ptr(new_lens), _ptr(new_free_count), _ptr(granted), _ptr(slots),
+            _stream(block_table)))
+    return new_owned, new_lens, new_free_count, granted, slots
+
+
+def trim_blocks(block_table, owned, keep_lens, free_blocks, free_count, new_owned=None,
+                new_free_count=None):
+    """Give back the blocks past ceil(keep_lens / 16) of every request (0: all of them);
+    returns (new_owned, new_free_count), int32.
+
+    The ids are pushed onto free_blocks (written in place); new_owned and
+    new_free_count may be owned and free_count themselves."""
+    r = (_native_module or _native()).trim_blocks(block_table, owned, keep_lens, free_blocks,
+                                                  free_count, new_owned, new_free_count)
+    if r is not None:
+        _raised(r)
+        return tuple(r)
+    _dev(block_table, torch.int32, "block_table")
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [bs][max_blocks]")
+    bs = block_table.shape[0]
+    owned, keep_lens = _i32s(bs, "owned", owned), _i32s(bs, "keep_lens", keep_lens)
+    _dev(free_blocks, torch.int32, "free_blocks")
+    free_count = _i32s(1, "free_count", free_count)
+    new_owned = _i32s(bs, "new_owned", new_owned, owned)
+    new_free_count = _i32s(1, "new_free_count", new_free_count, owned)
+    _same_device(block_table, owned=owned, keep_lens=keep_lens, free_blocks=free_blocks,
+                 free_count=free_count, new_owned=new_owned, new_free_count=new_free_count)
+    with torch.cuda.device(block_table.device):
+        _check("trim_blocks", lib().nsd_trim_blocks(
+            _ptr(block_table), block_table.shape[1], _ptr(owned), _ptr(keep_lens), bs,
+            _ptr(free_blocks), free_blocks.numel(), _ptr(free_count), _ptr(new_owned),
+            _ptr(new_free_count), _stream(block_table)))
+    return new_owned, new_free_count
+
+
+def _rows(t, name):
+    """[rows][heads][D] bf16 on the GPU, dense within a row; the rows' stride."""
+    if t.dtype != torch.bfloat16:
+        raise TypeError(f"{name} must be {torch.bfloat16}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on a GPU")
+    n, h, d = t.shape
+    if (h > 1 and t.stride(1) != d) or (d > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name}'s heads must be dense within a row")
+    return t.stride(0) if n > 1 else h * d
+
+
+def rope_append(k_pool, v_pool, q, k_new, v_new, positions, inv_freq, slots, sections=None,
+                interleaved=False, q_out=None):
+    """Rotary positions for the rows q [n][Hq][D] and k_new [n][Hkv][D], and k_new / v_new
+    into slots of one layer's pool; returns the turned queries (q_out, which may be q).
+
+    q, k_new, v_new: bf16, dense within a row; rows may be strided (views of a fused
+    projection's output).  positions: int32 [n] or [axes][n]; inv_freq: fp32 [rot/2], the
+    first rot dimensions of a head are turned; sections: how many of the pairs belong to each
+    axis (host integers; None for one axis); interleaved: pairs are (2i, 2i+1) instead of
+    (i, i + rot/2).  slots: int32 [n] as plan_blocks gives them; -1 leaves a row out of the
+    cache."""
+    r = (_native_module or _native()).rope_append(k_pool, v_pool, q, k_new, v_new, positions,
+                                                  inv_freq, slots, sections, interleaved, q_out)
+    if r is not None:
+        _raised(r)
+        return r
+    for t, n in ((q, "q"), (k_new, "k_new"), (v_new, "v_new")):
+        if t.dim() != 3:
+            raise ValueError(f"{n} must be [rows][heads][D]")
+    qs, ks, vs = _rows(q, "q"), _rows(k_new, "k_new"), _rows(v_new, "v_new")
+    _dev(k_pool, torch.bfloat16, "k_pool")
+    _dev(v_pool, torch.bfloat16, "v_pool")
+    n, hq, d = q.shape
+    hkv = k_new.shape[1]
+    nb = k_pool.shape[0]
+    if k_new.shape != (n, hkv, d) or v_new.shape != k_new.shape or d % 8 or \
+            k_pool.shape != (nb, hkv, d // 8, BLOCK_SIZE, 8) or \
+            v_pool.shape != (nb, hkv, d, BLOCK_SIZE):
+        raise ValueError("q, k_new, v_new and the pools do not match")
+    _dev(positions, torch.int32, "positions")
+    axes = 1 if positions.dim() == 1 else positions.shape[0]
+    if positions.dim() not in (1, 2) or positions.numel() != axes * n:
+        raise ValueError("positions must be [rows] or [axes][rows]")
+    _dev(inv_freq, torch.float32, "inv_freq")
+    if sections is None and axes > 1:
+        raise ValueError("several axes need sections")
+    if sections is not None and len(sections) != axes:
+        raise ValueError("one section per axis")
+    cuts = None if sections is None else (ctypes.c_int32 * axes)(*[int(s) for s in sections])
+    slots = _i32s(n, "slots", slots)
+    if q_out is None:
+        q_out = torch.empty((n, hq, d), dtype=q.dtype, device=q.device)
+    else:
+        _dev(q_out, torch.bfloat16, "q_out")
+        if q_out.shape != q.shape:
+            raise ValueError("q_out must have q's shape")
+    _same_device(q, k_pool=k_pool, v_pool=v_pool, k_new=k_new, v_new=v_new, positions=positions,
+                 inv_freq=inv_freq, slots=slots, q_out=q_out)
+    with torch.cuda.device(q.device):
+        _check("rope_append", lib().nsd_rope_append(
+            _ptr(k_pool), _ptr(v_pool), nb, _ptr(q), qs, _ptr(k_new), ks, _ptr(v_new), vs,
+            _ptr(positions), _ptr(inv_freq), cuts, axes, 2 * inv_freq.numel(), int(interleaved),
+            _ptr(slots), n, hq, hkv, BLOCK_SIZE, d, _ptr(q_out), _stream(q)))
+    return q_out
+
+
+def chunk_attention_workspace_size(bs, total_q, num_q_heads, num_kv_heads, head_dim, max_q_per_seq,
+                                   max_seq_len):
+    return int(lib().nsd_chunk_attention_workspace_size(bs, total_q, num_q_heads, num_kv_heads,
+                                                        head_dim, max_q_per_seq, max_seq_len))
+
+
+def chunk_attention(q, k_cache, v_cache, block_table, seq_lens, q_indptr, max_q_per_seq,
+                    max_seq_len, scale=None, softcap=0.0, slopes=None, first_keys=None,
+                    prefix_lens=None, out=None, workspace=None):
+    """Attention of each request's new tokens over its paged cache (one layer); returns out
+    [total_q][Hq][D] bf16.
+
+    Arguments as verify_attention, with any number of new tokens per request.  softcap: scores
+    become softcap * tanh(score / softcap) (0: none); slopes: fp32 [Hq], subtracted from a
+    score times the distance of query and key; first_keys: int32 [total_q], the first token each
+    query sees (a sliding window, a packed document); prefix_lens: int32 [bs], leading tokens
+    every query of the request sees.  workspace: chunk_attention_workspace_size(bs, total_q, ...)
+    bytes (allocated per call when None)."""
+    r = (_native_module or _native()).chunk_attention(
+        q, k_cache, v_cache, block_table, seq_lens, q_indptr, max_q_per_seq, max_seq_len, scale,
+        softcap, slopes, first_keys, prefix_lens, out, workspace)
+    if r is not None:
+        _raised(r)
+        return r
+    _dev(q, torch.bfloat16, "q")
+    _dev(k_cache, torch.bfloat16, "k_cache")
+    _dev(v_cache, torch.bfloat16, "v_cache")
+    if q.dim() != 3 or k_cache.dim() != 5:
+        raise ValueError("q must be [total_q][Hq][D], k_cache [blocks][Hkv][D/8][16][8]")
+    total_q, hq, d = q.shape
+    nb, hkv, dv8, bsz, vec = k_cache.shape
+    if dv8 * vec != d or vec != 8 or v_cache.shape != (nb, hkv, d, bsz):
+        raise ValueError("cache shapes do not match q")
+    _dev(seq_lens, torch.int32, "seq_lens")
+    bs = seq_lens.numel()
+    _dev(block_table, torch.int32, "block_table")
+    if block_table.dim() != 2 or block_table.shape[0] != bs:
+        raise ValueError("block_table / q_indptr do not match seq_lens")
+    q_indptr = _i32s(bs + 1, "q_indptr", q_indptr)
+    if slopes is not None:
+        _dev(slopes, torch.float32, "slopes")
+        if slopes.numel() != hq:
+            raise ValueError("slopes must have one entry per query head")
+    if first_keys is not None:
+        _i32s(total_q, "first_keys", first_keys)
+    if prefix_lens is not None:
+        _i32s(bs, "prefix_lens", prefix_lens)
+    if scale is None:
+        scale = 1.0 / math.sqrt(d)
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _dev(out, torch.bfloat16, "out")
+        if out.shape != q.shape:
+            raise ValueError("out must have q's shape")
+    need = chunk_attention_workspace_size(bs, total_q, hq, hkv, d, max_q_per_seq, max_seq_len)
+    workspace, ws_bytes = _attn_ws(workspace, need, q)
+    _same_device(q, k_cache=k_cache, v_cache=v_cache, block_table=block_table, seq_lens=seq_lens,
+                 q_indptr=q_indptr, slopes=slopes, first_keys=first_keys,
+                 prefix_lens=prefix_lens, out=out)
+    with torch.cuda.device(q.device):
+        _check("chunk_attention", lib().nsd_chunk_attention(
+            _ptr(q), _ptr(k_cache), _ptr(v_cache), nb, _ptr(block_table), block_table.shape[1],
+            _ptr(seq_lens), _ptr(q_indptr), bs, total_q, hq, hkv, d, bsz, max_q_per_seq,
+            max_seq_len, float(scale), float(softcap), _ptr(slopes), _ptr(first_keys),
+            _ptr(prefix_lens), _ptr(out), _ptr(workspace), ws_bytes, _stream(q)))
+    return out
+
+
 __all__ = ["lib", "version", "attention_waves", "check_plan", "check_pairs", "kv_gather", "verify_attention", "verify_attention_workspace_size",
            "new_workspace", "gather_verify_attention", "copy_plan", "COPY_H2D", "COPY_D2H",
            "DEFAULT_CHUNK", "kv_append", "commit_lengths", "host_alias", "kv_writeback",
-           "spec_accept", "spec_accept_static", "accept_workspace_size", "sample", "NsdError", "BLOCK_SIZE", "LIB_PATH"]
+           "spec_accept", "spec_accept_static", "accept_workspace_size", "sample", "plan_blocks",
+           "trim_blocks", "rope_append", "chunk_attention", "chunk_attention_workspace_size", "NsdError", "BLOCK_SIZE", "LIB_PATH"]

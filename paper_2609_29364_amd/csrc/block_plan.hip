@@ -1,0 +1,267 @@
+// Blocks of a step's new tokens: block tables, cache slots and the free list,
+// built on the device from the requests' lengths.
+//
+// Request r holds owned_r blocks and L_r tokens; n_r new tokens need
+//     need_r = max(0, ceil((L_r + n_r) / 16) - owned_r)
+// more.  Requests are served in order: with U_r the inclusive prefix sum of
+// the needs and F free ids, r is granted iff need_r = 0 or U_r <= F, and its
+// k-th new block is the free list's entry F - 1 - (U_r - need_r) - k (the list
+// is a stack whose top is its last entry).  As U does not fall, the granted
+// requests that need blocks are a prefix of those that do.  Trimming is the
+// inverse: the blocks past ceil(keep_r / 16) are pushed in request order.
+//
+// Both are a prefix sum over at most 8192 requests followed by independent
+// work per block or per token, bound by latency: a few launches' worth of
+// dependent loads (lengths, scan, search, id, store).  Every workgroup scans
+// the whole batch into LDS by itself (a few reads of at most 32 KiB arrays
+// from L2) rather than waiting for another launch's scan, then takes its share
+// of the tokens and blocks, each found by a binary search over the prefix in
+// LDS.  The new counters may be written over the old ones, which other
+// workgroups may still be reading: one workgroup writes them after its own
+// scan, and several leave aliased ones to a second launch.
+#include "nsd_internal.h"
+
+namespace {
+
+constexpr int kThreads = 1024;
+constexpr int kMaxBatch = 8192;
+constexpr int kPer = kMaxBatch / kThreads;   // requests per thread, at most
+
+// Inclusive prefix sum over the workgroup's threads.
+__device__ inline int64_t scan(int64_t x, int64_t* part) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) {
+    const int64_t y = __shfl_up(x, s);
+    if (lane >= s) x += y;
+  }
+  if (lane == 63) part[wave] = x;
+  __syncthreads();
+  int64_t before = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) before += w < wave ? part[w] : 0;
+  return x + before;
+}
+
+// The last r in [0, n) with key[r] <= x, for a key that does not fall and key[0] <= x.
+__device__ inline int find(const int32_t* key, int n, int x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (key[mid] <= x) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+struct PlanArgs {
+  int32_t* table;
+  const int32_t *owned, *lens, *indptr, *free_ids, *free_count;
+  int32_t *new_owned, *new_lens, *new_count, *granted, *slots;
+  int32_t width, capacity, bs, total_q;
+};
+
+// LDS: indptr, start, lens, owned, each of bs + 1 entries.
+__global__ __launch_bounds__(kThreads) void plan_kernel(PlanArgs A, int counters, int rows) {
+  extern __shared__ int32_t mem[];
+  __shared__ int64_t part[kThreads / 64];
+  __shared__ int32_t used;
+  const int n = A.bs, tid = threadIdx.x;
+  int32_t *indptr = mem, *start = mem + (n + 1), *lens = mem + 2 * (n + 1),
+          *owned = mem + 3 * (n + 1);
+  const int per = (n + kThreads - 1) / kThreads;
+  const int free_n = min(max(A.free_count[0], 0), A.capacity);
+  if (tid == 0) used = 0;
+  int64_t need[kPer], sum = 0;
+  bool wide[kPer];   // more tokens than the table's row holds
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int r = tid * per + i;
+    need[i] = 0;
+    wide[i] = false;
+    if (i >= per || r >= n) continue;
+    const int a = min(max(A.indptr[r], 0), A.total_q);
+    const int b = min(max(A.indptr[r + 1], a), A.total_q);
+    const int l = max(A.lens[r], 0), o = min(max(A.owned[r], 0), A.width);
+    const int64_t blocks = ((int64_t)l + (b - a) + NSD_BLOCK_SIZE - 1) / NSD_BLOCK_SIZE;
+    indptr[r] = a;
+    lens[r] = l;
+    owned[r] = o;
+    wide[i] = blocks > A.width;
+    need[i] = wide[i] ? 0 : max(blocks - o, (int64_t)0);
+    sum += need[i];
+  }
+  int64_t upto = scan(sum, part) - sum;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int r = tid * per + i;
+    if (i >= per || r >= n) continue;
+    const int64_t before = upto;
+    upto += need[i];
+    const bool ok = !wide[i] && (need[i] == 0 || upto <= free_n);
+    // past the granted requests the prefix stays above every granted block's number
+    start[r] = (int32_t)min(before, (int64_t)free_n);
+    if (ok && need[i]) atomicMax(&used, (int32_t)upto);
+    if (counters && blockIdx.x == 0) {
+      const int count = min(max(A.indptr[r + 1], indptr[r]), A.total_q) - indptr[r];
+      A.granted[r] = ok;
+      A.new_owned[r] = owned[r] + (ok ? (int32_t)need[i] : 0);
+      A.new_lens[r] = lens[r] + (ok ? count : 0);
+    }
+    if (!ok) owned[r] = -1;
+  }
+  __syncthreads();
+  if (counters && blockIdx.x == 0 && tid == 0) A.new_count[0] = free_n - used;
+  if (!rows) return;
+  const int at = blockIdx.x * kThreads + tid, step = gridDim.x * kThreads;
+  for (int k = at; k < used; k += step) {
+    // the last request whose first new block is at most the k-th: it holds the block
+    // (a request without new blocks shares its start with the next one that has some)
+    const int r = find(start, n, k);
+    A.table[(int64_t)r * A.width + owned[r] + (k - start[r])] = A.free_ids[free_n - 1 - k];
+  }
+  for (int i = at; i < A.total_q; i += step) {
+    const int r = find(indptr, n, i);
+    int32_t slot = -1;
+    const int64_t t = (int64_t)lens[r] + (i - indptr[r]), b = t / NSD_BLOCK_SIZE;
+    // a granted request's tokens lie within its row; offsets that are no prefix sum need not
+    if (owned[r] >= 0 && t >= 0 && b < A.width) {
+      const int64_t k = start[r] + (b - owned[r]);
+      const int id = b < owned[r] ? A.table[(int64_t)r * A.width + b]
+                     : k < free_n ? A.free_ids[free_n - 1 - k] : -1;
+      if (id >= 0 && id < (1 << 27)) slot = id * NSD_BLOCK_SIZE + (int)(t % NSD_BLOCK_SIZE);
+    }
+    A.slots[i] = slot;
+  }
+}
+
+struct TrimArgs {
+  const int32_t *table, *owned, *keep;
+  int32_t* free_ids;
+  const int32_t* free_count;
+  int32_t *new_owned, *new_count;
+  int32_t width, capacity, bs;
+};
+
+// LDS: start, kept, each of bs + 1 entries.
+__global__ __launch_bounds__(kThreads) void trim_kernel(TrimArgs A, int counters, int rows) {
+  extern __shared__ int32_t mem[];
+  __shared__ int64_t part[kThreads / 64];
+  __shared__ int32_t total;
+  const int n = A.bs, tid = threadIdx.x;
+  int32_t *start = mem, *kept = mem + (n + 1);
+  const int per = (n + kThreads - 1) / kThreads;
+  const int free_n = min(max(A.free_count[0], 0), A.capacity);
+  int32_t back[kPer];
+  int64_t sum = 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int r = tid * per + i;
+    back[i] = 0;
+    if (i >= per || r >= n) continue;
+    const int o = min(max(A.owned[r], 0), A.width);
+    const int64_t b = ((int64_t)max(A.keep[r], 0) + NSD_BLOCK_SIZE - 1) / NSD_BLOCK_SIZE;
+    const int k = (int)min((int64_t)o, b);
+    kept[r] = k;
+    back[i] = o - k;
+    sum += back[i];
+  }
+  const int64_t end = scan(sum, part);
+  int64_t upto = end - sum;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int r = tid * per + i;
+    if (i >= per || r >= n) continue;
+    start[r] = (int32_t)upto;
+    upto += back[i];
+    if (counters && blockIdx.x == 0) A.new_owned[r] = kept[r];
+  }
+  // ids past the list's capacity are dropped
+  if (tid == kThreads - 1) total = (int32_t)min(end, (int64_t)(A.capacity - free_n));
+  __syncthreads();
+  if (counters && blockIdx.x == 0 && tid == 0) A.new_count[0] = free_n + total;
+  if (!rows) return;
+  for (int k = blockIdx.x * kThreads + tid; k < total; k += gridDim.x * kThreads) {
+    const int r = find(start, n, k);
+    A.free_ids[free_n + k] = A.table[(int64_t)r * A.width + kept[r] + (k - start[r])];
+  }
+}
+
+// Workgroups for `work` blocks and tokens: one where its threads take at most four each.
+int groups(int64_t work) {
+  const int64_t g = work <= 4 * kThreads ? 1 : (work + 2 * kThreads - 1) / (2 * kThreads);
+  return (int)(g < 256 ? g : 256);
+}
+
+// Runs kernel(args, counters, rows) over the work, the counters in the same launch unless
+// several workgroups would still read what they overwrite.
+template <class Kernel, class Args>
+void launch(Kernel kernel, const Args& args, int64_t work, bool alias, size_t lds,
+            hipStream_t stream) {
+  const int g = groups(work);
+  const bool apart = g > 1 && alias;
+  hipLaunchKernelGGL(kernel, dim3(g), dim3(kThreads), lds, stream, args, apart ? 0 : 1, 1);
+  if (apart)
+    hipLaunchKernelGGL(kernel, dim3(1), dim3(kThreads), lds, stream, args, 1, 0);
+}
+
+nsd_status check_sizes(const char* fn, int32_t bs, int32_t width, int32_t capacity) {
+  using namespace nsd;
+  if (bs < 0 || bs > kMaxBatch)
+    return fail(NSD_ERR_SHAPE, "%s: bs must be in [0, %d]", fn, kMaxBatch);
+  if (width < 1 || capacity < 0)
+    return fail(NSD_ERR_SHAPE, "%s: max_blocks_per_seq < 1 or free_capacity < 0", fn);
+  if (capacity > (1 << 27))
+    return fail(NSD_ERR_UNSUPPORTED, "%s: a pool of more than 2^27 blocks", fn);
+  return NSD_OK;
+}
+
+}  // namespace
+
+extern "C" nsd_status nsd_plan_blocks(int32_t* block_table, int32_t max_blocks_per_seq,
+                                      const int32_t* owned, const int32_t* seq_lens,
+                                      const int32_t* q_indptr, int32_t bs, int32_t total_q,
+                                      const int32_t* free_blocks, int32_t free_capacity,
+                                      const int32_t* free_count, int32_t* new_owned,
+                                      int32_t* new_lens, int32_t* new_free_count,
+                                      int32_t* granted, int32_t* slots, void* stream) {
+  using namespace nsd;
+  const char* fn = "plan_blocks";
+  if (const nsd_status st = check_sizes(fn, bs, max_blocks_per_seq, free_capacity)) return st;
+  if (total_q < 0) return fail(NSD_ERR_SHAPE, "%s: total_q < 0", fn);
+  if (!free_count || !new_free_count || (free_capacity && !free_blocks) ||
+      (bs && (!block_table || !owned || !seq_lens || !q_indptr || !new_owned || !new_lens ||
+              !granted)) || (bs && total_q && !slots))
+    return fail(NSD_ERR_NULL, "%s: NULL pointer argument", fn);
+  const PlanArgs args{block_table, owned,     seq_lens,       q_indptr, free_blocks, free_count,
+                      new_owned,   new_lens,  new_free_count, granted,  slots,       max_blocks_per_seq,
+                      free_capacity, bs, bs ? total_q : 0};
+  const bool alias = new_owned == owned || new_lens == seq_lens || new_free_count == free_count;
+  clear_stale_error();
+  launch(plan_kernel, args, args.total_q, alias, ((size_t)bs + 1) * 16, (hipStream_t)stream);
+  return check_launch(fn);
+}
+
+extern "C" nsd_status nsd_trim_blocks(const int32_t* block_table, int32_t max_blocks_per_seq,
+                                      const int32_t* owned, const int32_t* keep_lens, int32_t bs,
+                                      int32_t* free_blocks, int32_t free_capacity,
+                                      const int32_t* free_count, int32_t* new_owned,
+                                      int32_t* new_free_count, void* stream) {
+  using namespace nsd;
+  const char* fn = "trim_blocks";
+  if (const nsd_status st = check_sizes(fn, bs, max_blocks_per_seq, free_capacity)) return st;
+  if (!free_count || !new_free_count || (free_capacity && !free_blocks) ||
+      (bs && (!block_table || !owned || !keep_lens || !new_owned)))
+    return fail(NSD_ERR_NULL, "%s: NULL pointer argument", fn);
+  if ((int64_t)bs * max_blocks_per_seq > INT32_MAX)
+    return fail(NSD_ERR_UNSUPPORTED, "%s: a block table of more than 2^31-1 entries", fn);
+  const TrimArgs args{block_table, owned,     keep_lens,      free_blocks, free_count,
+                      new_owned,   new_free_count, max_blocks_per_seq, free_capacity, bs};
+  const bool alias = new_owned == owned || new_free_count == free_count;
+  clear_stale_error();
+  // the host does not know how many blocks come back: at most the tables' or the list's
+  const int64_t most = (int64_t)bs * max_blocks_per_seq;
+  launch(trim_kernel, args, most < free_capacity ? most : free_capacity, alias,
+         ((size_t)bs + 1) * 8, (hipStream_t)stream);
+  return check_launch(fn);
+}

@@ -1,0 +1,609 @@
+// Attention of each request's new tokens (a prompt chunk, or one token) over
+// its paged cache.
+//
+// Query row (token j, head h) of request r sits at position p = L_r - n_r + j
+// and sees token t iff t < prefix_r, or first_j <= t <= p (first_j = 0 where no
+// first keys are given), in a block whose id is valid:
+//     x_t = f(scale <q, k_t>) - slope_h |p - t|,  f(x) = cap tanh(x / cap) or x
+//     o   = sum_t e^(x_t - m) v_t / sum_t e^(x_t - m),  m = max_t x_t
+// in one pass over the tokens with the running maximum and sum in fp32.
+//
+// The (query tokens x heads of a group) rows of one KV head are one product's
+// columns: S^T = K Q^T and O^T = V^T P^T on 32x32x16 bf16 MFMAs.  A workgroup
+// of four waves takes 128 rows, 32 a wave, whose Q operands stay in registers;
+// stages of 64 tokens (four blocks) go to LDS by direct loads, double-buffered,
+// and serve all four waves.  Two workgroups share a CU, so one's softmax runs
+// under the other's MFMAs.  The cache's layout feeds the MFMAs as it is: a K
+// operand is 16 bytes of one slot (8 dimensions), a V^T operand 16 bytes of one
+// dimension (8 slots).  The K rows enter with bits 2 and 3 of their slot
+// swapped, which makes the eight S^T values a lane holds of a block those of
+// the 8 slots its V^T operand has: P^T goes from accumulator to operand
+// (rounded to bf16, an error of at most 2^-9 of each weight) without leaving
+// its lane.
+//
+// The softmax rescale is skipped while no row's maximum grows by more than 2^8
+// (weights then stay below 2^8, far from any limit of fp32).  Tokens hidden
+// from a row get weight 0; as 0 times an infinity or NaN is NaN, a V operand of
+// a stage with hidden tokens is looked through for them, and where one has any
+// they are taken out of the product and added to the rows that see them.
+#include "nsd_internal.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+
+constexpr int kMaxBatch = 8192;
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kWaveRows = 32;
+constexpr int kRows = kWaves * kWaveRows;    // query rows (token, head of the group) of an item
+constexpr int kStage = 64;                   // tokens of a stage
+constexpr int kStageBlocks = kStage / NSD_BLOCK_SIZE;
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kSlack = 8.f;                // log2 of the weights' bound
+
+struct Params {
+  const uint16_t* q;
+  const uint16_t *k, *v;
+  const int32_t* first;
+  const float* slopes;
+  uint16_t* out;
+  float* part;        // [splits][rows][D] normalised partial rows, then [splits][rows][2] (max, sum)
+  int64_t num_blocks;
+  int64_t rows;       // total_q * hq
+  float scale, cap;   // scale >= 0 (a negative one is in `negate`)
+  uint32_t negate;    // 0x80008000: Q's signs are flipped
+  int32_t width, bs, total_q, hq, hkv, group, max_len, items, splits;
+};
+
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+__device__ inline uint32_t pack(float a, float b) {
+  const bf16x2 v = __builtin_convertvector(f32x2{a, b}, bf16x2);
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// x of the lane 32 away (a register swapped with a copy of itself holds both halves' values).
+__device__ inline float other_half(float x) {
+  uint32_t a = __float_as_uint(x), b = a;
+  asm volatile("s_nop 1\n\tv_permlane32_swap_b32 %0, %1\n\ts_nop 1" : "+v"(a), "+v"(b));
+  return __uint_as_float((threadIdx.x & 32) ? a : b);
+}
+
+// The first item of request r: its rows' tiles are items first_item(r) .. first_item(r + 1) - 1,
+// which are at least ceil(rows / kRows) of them whatever the rows, so no prefix sum is needed.
+__device__ inline int first_item(const Params& P, const int32_t* indptr, int r) {
+  const int64_t a = min(max(indptr[r], 0), P.total_q);
+  return (int)(a * P.group / kRows) + r;
+}
+
+// The last request whose first item is at most `item`, by 64 lanes' probes a round.
+__device__ inline int find_request(const Params& P, const int32_t* indptr, int item) {
+  int lo = 0, n = P.bs;
+  while (n > 1) {
+    const int step = (n + 63) / 64, i = lo + (int)(threadIdx.x & 63) * step;
+    const bool in = i < lo + n && (i == lo || first_item(P, indptr, i) <= item);
+    const uint64_t m = __ballot(in);
+    const int last = 63 - __builtin_clzll(m);
+    n = min(step, n - last * step);
+    lo += last * step;
+  }
+  return uniform(lo);
+}
+
+// 16 bytes a lane from `src` (its own address) to 1 KiB at `dst`, a lane's at lane * 16.
+__device__ inline void load_lds(const void* src, void* dst) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)src,
+                                   (__attribute__((address_space(3))) uint32_t*)dst, 16, 0, 0);
+}
+
+template <int D>
+struct Acc {
+  f32x16 o[D / 32];   // O^T: row of the wave = lane % 32, dimension 32 t + 8 (i / 4) + 4 (lane / 32) + i % 4
+  float m, l;         // running maximum (log2 domain) and this lane's sum
+};
+
+// One row's mask: what its position, first key and prefix let it see.
+struct Sight {
+  int p, first, prefix;
+  float slope;   // log2 domain
+};
+
+// D: head dimension; CAP: capped scores; BIAS: slopes; MASK: first keys or prefixes given.
+template <int D, bool CAP, bool BIAS>
+struct Tile {
+  static constexpr int kHalf = D * 16;   // elements of a block's K or V tile
+
+  // S^T of 32 tokens x 32 rows.  k: two blocks' tiles [D/8][16][8].
+  static __device__ inline f32x16 scores(const uint16_t* k, const bf16x8 (&q)[D / 16]) {
+    const int lane = threadIdx.x & 63, r = lane & 15;
+    const int slot = (r & 3) | (r & 4) << 1 | (r & 8) >> 1;
+    const uint16_t* p = k + (lane >> 4 & 1) * kHalf + (lane >> 5) * 128 + slot * 8;
+    f32x16 s = {};
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk)
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*(const bf16x8*)(p + kk * 256), q[kk], s, 0, 0, 0);
+    return s;
+  }
+
+  // V^T operand of block b's dimensions 32 t ..: [D][16] as it is in the cache.
+  static __device__ inline bf16x8 values(const uint16_t* v, int b, int t) {
+    const int lane = threadIdx.x & 63;
+    return *(const bf16x8*)(v + b * kHalf + (t * 32 + (lane & 31)) * 16 + (lane >> 5) * 8);
+  }
+};
+
+// bf16 pairs whose exponent is all ones.
+__device__ inline bool unusual(uint32_t w) {
+  return ((w & 0x7f80u) == 0x7f80u) | ((w & 0x7f800000u) == 0x7f800000u);
+}
+
+// One stage of NSUB x 32 tokens from t0 on for a wave's rows.  hidden: some row may not see
+// some token.  valid: bit b set if block b of the stage may be read.
+template <int D, bool CAP, bool BIAS, int NSUB>
+__device__ inline void stage(Acc<D>& a, const uint16_t* k, const uint16_t* v,
+                             const bf16x8 (&q)[D / 16], const Params& P, const Sight& w, int t0,
+                             uint32_t valid, bool hidden) {
+  using T = Tile<D, CAP, BIAS>;
+  const int half = (threadIdx.x & 63) >> 5;
+  f32x16 s[NSUB];
+#pragma unroll
+  for (int u = 0; u < NSUB; ++u) s[u] = T::scores(k + u * 2 * T::kHalf, q);
+  const float c = P.scale * kLog2e;
+  if constexpr (CAP || BIAS) {
+    const float y = CAP ? 2.f * c / P.cap : 0.f, top = P.cap * kLog2e;
+    const float d0 = (float)(w.p - t0 - 8 * half);
+#pragma unroll
+    for (int u = 0; u < NSUB; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float x;
+        if constexpr (CAP) {
+          // cap tanh(x / cap): 1 - 2 / (1 + e^(2 x / cap))
+          const float e = __builtin_amdgcn_exp2f(s[u][i] * y);
+          x = fmaf(-2.f * top, __builtin_amdgcn_rcpf(1.f + e), top);
+        } else {
+          x = s[u][i] * c;
+        }
+        if constexpr (BIAS) x = fmaf(-w.slope, fabsf(d0 - (float)(u * 32 + i / 8 * 16 + i % 8)), x);
+        s[u][i] = x;
+      }
+  }
+  constexpr bool kLog2 = CAP || BIAS;   // scores are in the log2 domain already
+  uint32_t seen[NSUB];                  // a bit per token of this lane
+  if (hidden) {
+#pragma unroll
+    for (int u = 0; u < NSUB; ++u) {
+      seen[u] = 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int t = t0 + u * 32 + i / 8 * 16 + half * 8 + i % 8;
+        const int block_ok = valid >> (u * 2 + i / 8) & 1;
+        const bool on = block_ok & ((t < w.prefix) | ((t <= w.p) & (t >= w.first)));
+        seen[u] |= on ? 1u << i : 0u;
+        s[u][i] = on ? s[u][i] : -INFINITY;
+      }
+    }
+  }
+  float top = s[0][0];
+#pragma unroll
+  for (int u = 0; u < NSUB; ++u)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
+  top = fmaxf(top, other_half(top));
+  if constexpr (!kLog2) top *= c;
+  if (c == 0.f && !kLog2) top = top == top ? top : -INFINITY;   // 0 times a hidden -inf
+  if (__ballot(top > a.m + kSlack || a.m == -INFINITY)) {
+    const float m = fmaxf(a.m, top);
+    const float f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(a.m - m);
+    a.m = m;
+    a.l *= f;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) a.o[t][i] *= f;
+  }
+  const float sub = a.m == -INFINITY ? 0.f : a.m;
+  u32x4 p[NSUB * 2];
+#pragma unroll
+  for (int u = 0; u < NSUB; ++u)
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      float e[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        e[j] = __builtin_amdgcn_exp2f(kLog2 ? s[u][i + j] - sub : fmaf(s[u][i + j], c, -sub));
+        if (hidden) e[j] = seen[u] >> (i + j) & 1 ? e[j] : 0.f;
+        a.l += e[j];
+      }
+      p[u * 2 + i / 8][i % 8 / 2] = pack(e[0], e[1]);
+    }
+#pragma unroll
+  for (int b = 0; b < NSUB * 2; ++b) {
+    bf16x8 vt[D / 32];
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) vt[t] = T::values(v, b, t);
+    if (hidden) {
+      bool odd = false;
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t) {
+        const u32x4 x = __builtin_bit_cast(u32x4, vt[t]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) odd |= unusual(x[e]);
+      }
+      if (__ballot(odd)) {
+        // infinities and NaN leave the product; the rows that see one get it added: the number
+        // of +infinities or NaN a row sees, and of -infinities or NaN, as products of flags
+        u32x4 flags;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t bits = seen[b / 2] >> (b % 2 * 8 + 2 * e);
+          flags[e] = (bits & 1 ? 0x3f80u : 0u) | (bits & 2 ? 0x3f800000u : 0u);
+        }
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) {
+          u32x4 x = __builtin_bit_cast(u32x4, vt[t]), up, down;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            up[e] = down[e] = 0;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const uint32_t h = x[e] >> (16 * j) & 0xffffu;
+              const bool big = (h & 0x7f80u) == 0x7f80u, nan = big && (h & 0x7fu);
+              if (big && (nan || !(h & 0x8000u))) up[e] |= 0x3f80u << (16 * j);
+              if (big && (nan || (h & 0x8000u))) down[e] |= 0x3f80u << (16 * j);
+              if (big) x[e] &= ~(0xffffu << (16 * j));
+            }
+          }
+          vt[t] = __builtin_bit_cast(bf16x8, x);
+          const bf16x8 see = __builtin_bit_cast(bf16x8, flags);
+          f32x16 n = {};
+          n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, up), see, n, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) a.o[t][i] += n[i] > 0.f ? INFINITY : 0.f;
+          n = f32x16{};
+          n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, down), see, n, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) a.o[t][i] -= n[i] > 0.f ? INFINITY : 0.f;
+        }
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+      a.o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt[t], __builtin_bit_cast(bf16x8, p[b]),
+                                                       a.o[t], 0, 0, 0);
+  }
+}
+
+template <int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
+    const Params P, const int32_t* __restrict__ tables, const int32_t* __restrict__ lens,
+    const int32_t* __restrict__ indptr, const int32_t* __restrict__ prefixes) {
+  constexpr int kTile = D * 16;                     // elements of a block's K or V tile
+  constexpr int kPlane = kStageBlocks * kTile;      // of a stage's K or V
+  __shared__ __attribute__((aligned(16))) uint16_t buf0[2 * kPlane], buf1[2 * kPlane];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  // heads fastest: with 8 KV heads the workgroups of a head share an XCD's L2
+  const int x = blockIdx.x, g = x % P.hkv;
+  const int split = x / P.hkv % P.splits;
+  // a request's last items see the most tokens: they start first
+  const int item = P.items - 1 - x / P.hkv / P.splits;
+  const int r = find_request(P, indptr, item);
+  const int a0 = min(max(indptr[r], 0), P.total_q);
+  const int a1 = min(max(indptr[r + 1], a0), P.total_q);
+  const int n = a1 - a0;
+  const int64_t rows = (int64_t)n * P.group;
+  const int64_t row0 = (int64_t)(item - first_item(P, indptr, r)) * kRows;
+  if (row0 < 0 || row0 >= rows) return;
+  const int L = min(max(lens[r], 0),
+                    min(P.max_len, P.width < (1 << 26) ? P.width * 16 : 1 << 30));
+  const int last = L - 1;
+  const int prefix = prefixes ? min(max(prefixes[r], 0), L) : 0;
+
+  // this lane's row
+  const int64_t row = row0 + wave * kWaveRows + (lane & 31);
+  const bool mine = row < rows;
+  const int j = mine ? (int)(row / P.group) : 0, h = mine ? (int)(row - (int64_t)j * P.group) : 0;
+  Sight w;
+  w.p = mine ? min(L - n + j, last) : -1;
+  w.first = mine && P.first ? P.first[a0 + j] : 0;
+  w.prefix = mine ? prefix : 0;
+  w.slope = BIAS && mine ? P.slopes[g * P.group + h] * kLog2e : 0.f;
+  bf16x8 q[D / 16];
+  {
+    const uint16_t* src = P.q + ((int64_t)(a0 + j) * P.hq + g * P.group + h) * D + (lane >> 5) * 8;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+      u32x4 t = {};
+      if (mine) t = *(const u32x4*)(src + kk * 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) t[e] ^= P.negate;
+      q[kk] = __builtin_bit_cast(bf16x8, t);
+    }
+  }
+  // what the wave's rows, and the workgroup's, see: positions and first keys at the extremes
+  int pmin = mine ? w.p : INT32_MAX, fmax = mine ? w.first : INT32_MIN, fmin = mine ? w.first : INT32_MAX;
+#pragma unroll
+  for (int s = 1; s < 32; s *= 2) {
+    pmin = min(pmin, __shfl_xor(pmin, s));
+    fmax = max(fmax, __shfl_xor(fmax, s));
+    fmin = min(fmin, __shfl_xor(fmin, s));
+  }
+  pmin = uniform(pmin);
+  fmax = uniform(fmax);
+  fmin = uniform(fmin);
+  const int64_t wave_last = min(rows, row0 + (wave + 1) * kWaveRows) - 1;
+  const int pmax = wave_last >= row0 + wave * kWaveRows
+                       ? min(L - n + (int)(wave_last / P.group), last) : -1;
+  int from = 0;   // the workgroup's first key
+  if (P.first) {
+    int32_t* at = (int32_t*)buf0;
+    if (lane == 0) at[wave] = fmin;
+    __syncthreads();
+    from = max(min(min(at[0], at[1]), min(at[2], at[3])), 0);
+    from = uniform(from);
+    __syncthreads();
+  }
+  const int to = min(L - n + (int)((min(rows, row0 + kRows) - 1) / P.group), last) + 1;   // past its last key
+  // stages: those of the prefix, then from the first key's on
+  const int n1 = (prefix + kStage - 1) / kStage;
+  const int s2 = max(n1, from / kStage);
+  const int n2 = to > 0 ? max((to + kStage - 1) / kStage - s2, 0) : 0;
+  const int stages = n1 + n2;
+  const int per = (stages + P.splits - 1) / P.splits;
+  const int i0 = min(split * per, stages), i1 = min(i0 + per, stages);
+
+  Acc<D> a;
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t) a.o[t] = f32x16{};
+  a.m = -INFINITY;
+  a.l = 0.f;
+
+  const int32_t* table = tables + (int64_t)r * P.width;
+  const int blocks = (L + 15) / 16;
+  auto start = [&](int i) { return (i < n1 ? i : i - n1 + s2) * kStage; };
+  // which blocks of a stage may be read
+  auto validity = [&](int t0) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int b = 0; b < kStageBlocks; ++b) {
+      const int id = table[min(t0 / 16 + b, blocks - 1)];
+      m |= (t0 / 16 + b < blocks) & (id >= 0) & (id < P.num_blocks) ? 1u << b : 0u;
+    }
+    return m;
+  };
+  // wave w loads block w of the stage; an invalid one's place gets block 0
+  auto load = [&](int t0, uint16_t* buf) {
+    const int b = min(t0 / 16 + wave, blocks - 1);
+    int id = table[b];
+    id = id >= 0 && id < P.num_blocks ? id : 0;
+    const int64_t at = ((int64_t)id * P.hkv + g) * kTile + lane * 8;
+#pragma unroll
+    for (int c = 0; c < kTile / 512; ++c) {
+      load_lds(P.k + at + c * 512, buf + wave * kTile + c * 512);
+      load_lds(P.v + at + c * 512, buf + kPlane + wave * kTile + c * 512);
+    }
+  };
+  auto step = [&](int i, uint16_t* now, uint16_t* next) {
+    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): this wave's part of the stage is in LDS
+    __syncthreads();
+    if (i + 1 < i1) load(start(i + 1), next);
+    const int t0 = start(i);
+    const bool any = pmax >= 0 && ((t0 <= pmax && t0 + kStage > fmin) || t0 < prefix);
+    if (any) {
+      const uint32_t valid = validity(t0);
+      const bool all = valid == (1u << kStageBlocks) - 1 &&
+                       ((t0 + kStage - 1 <= pmin && t0 >= fmax) || t0 + kStage <= prefix);
+      if (all)
+        stage<D, CAP, BIAS, 2>(a, now, now + kPlane, q, P, w, t0, valid, false);
+      else
+        for (int u = 0; u < 2; ++u)
+          stage<D, CAP, BIAS, 1>(a, now + u * 2 * kTile, now + kPlane + u * 2 * kTile, q, P, w,
+                                 t0 + u * 32, valid >> (2 * u) & 3, true);
+    }
+  };
+  if (i0 < i1) load(start(i0), buf0);
+  for (int i = i0; i < i1; i += 2) {
+    step(i, buf0, buf1);
+    if (i + 1 < i1) step(i + 1, buf1, buf0);
+  }
+
+  if (!mine) return;
+  const float l = a.l + other_half(a.l);
+  const float f = l == 0.f ? 0.f : 1.f / l;   // no visible token: 0
+  const int64_t out_row = (int64_t)(a0 + j) * P.hq + g * P.group + h;
+  if (P.splits == 1) {
+    uint16_t* dst = P.out + out_row * D + (lane >> 5) * 4;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        u32x2 y;
+        y[0] = pack(a.o[t][4 * c] * f, a.o[t][4 * c + 1] * f);
+        y[1] = pack(a.o[t][4 * c + 2] * f, a.o[t][4 * c + 3] * f);
+        *(u32x2*)(dst + t * 32 + c * 8) = y;
+      }
+    return;
+  }
+  float* dst = P.part + ((int64_t)split * P.rows + out_row) * D + (lane >> 5) * 4;
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      float4 y = {a.o[t][4 * c] * f, a.o[t][4 * c + 1] * f, a.o[t][4 * c + 2] * f, a.o[t][4 * c + 3] * f};
+      *(float4*)(dst + t * 32 + c * 8) = y;
+    }
+  if (lane < 32) {
+    float2* ml = (float2*)(P.part + (int64_t)P.splits * P.rows * D) + (int64_t)split * P.rows + out_row;
+    *ml = make_float2(a.m, l);
+  }
+}
+
+// The splits of each row joined: D/4 threads a row.
+template <int D>
+__global__ __launch_bounds__(256) void join_kernel(const float* part, uint16_t* out, int64_t rows,
+                                                   int splits) {
+  const int64_t row = (int64_t)blockIdx.x * (1024 / D) + threadIdx.x / (D / 4);
+  const int c = threadIdx.x % (D / 4);
+  if (row >= rows) return;
+  const float2* ml = (const float2*)(part + (int64_t)splits * rows * D);
+  float m = -INFINITY;
+  for (int s = 0; s < splits; ++s) m = fmaxf(m, ml[s * rows + row].x);
+  float sum = 0.f;
+  float4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < splits; ++s) {
+    const float2 x = ml[s * rows + row];
+    if (x.y == 0.f) continue;   // this split saw nothing
+    const float f = __builtin_amdgcn_exp2f(x.x - m) * x.y;
+    const float4 y = *(const float4*)(part + (s * rows + row) * D + c * 4);
+    sum += f;
+    o.x += f * y.x;
+    o.y += f * y.y;
+    o.z += f * y.z;
+    o.w += f * y.w;
+  }
+  const float f = sum == 0.f ? 0.f : 1.f / sum;
+  u32x2 y;
+  y[0] = pack(o.x * f, o.y * f);
+  y[1] = pack(o.z * f, o.w * f);
+  *(u32x2*)(out + row * D + c * 4) = y;
+}
+
+// Items of a batch (an upper bound) and the splits of their tokens.
+struct Plan {
+  int64_t items;
+  int splits;
+};
+
+Plan plan(int32_t bs, int32_t total_q, int32_t hq, int32_t hkv, int32_t max_len) {
+  Plan p;
+  p.items = (int64_t)total_q * (hq / hkv) / kRows + bs;
+  const int64_t groups = p.items * hkv, stages = ((int64_t)max_len + kStage - 1) / kStage;
+  // two workgroups a CU, at least four stages a split
+  int64_t s = std::min<int64_t>(512 / std::max<int64_t>(groups, 1), stages / 4);
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(s, 64));
+  return p;
+}
+
+bool sizes_ok(int32_t bs, int32_t total_q, int32_t hq, int32_t hkv, int32_t d, int32_t max_q,
+              int32_t max_len) {
+  return bs >= 0 && bs <= kMaxBatch && total_q >= 0 && hkv >= 1 && hq >= hkv && hq % hkv == 0 &&
+         (d == 64 || d == 128) && max_q >= 1 && max_len >= 1 &&
+         (int64_t)total_q * hq <= INT32_MAX;
+}
+
+size_t workspace_bytes(const Plan& p, int32_t total_q, int32_t hq, int32_t d) {
+  return p.splits == 1 ? 0 : (size_t)p.splits * total_q * hq * (d + 2) * sizeof(float);
+}
+
+}  // namespace
+
+extern "C" size_t nsd_chunk_attention_workspace_size(int32_t bs, int32_t total_q,
+                                                     int32_t num_q_heads, int32_t num_kv_heads,
+                                                     int32_t head_dim, int32_t max_q_per_seq,
+                                                     int32_t max_seq_len) {
+  if (!sizes_ok(bs, total_q, num_q_heads, num_kv_heads, head_dim, max_q_per_seq, max_seq_len))
+    return 0;
+  return workspace_bytes(plan(bs, total_q, num_q_heads, num_kv_heads, max_seq_len), total_q,
+                         num_q_heads, head_dim);
+}
+
+extern "C" nsd_status nsd_chunk_attention(
+    const void* q, const void* k_cache, const void* v_cache, int64_t num_blocks,
+    const int32_t* block_table, int32_t max_blocks_per_seq, const int32_t* seq_lens,
+    const int32_t* q_indptr, int32_t bs, int32_t total_q, int32_t num_q_heads,
+    int32_t num_kv_heads, int32_t head_dim, int32_t block_size, int32_t max_q_per_seq,
+    int32_t max_seq_len, float scale, float softcap, const float* slopes,
+    const int32_t* first_keys, const int32_t* prefix_lens, void* out, void* workspace,
+    size_t workspace_size, void* stream) {
+  using namespace nsd;
+  const char* fn = "chunk_attention";
+  if (bs < 0 || bs > kMaxBatch)
+    return fail(NSD_ERR_SHAPE, "%s: bs must be in [0, %d]", fn, kMaxBatch);
+  if (block_size != NSD_BLOCK_SIZE)
+    return fail(NSD_ERR_UNSUPPORTED, "%s: block_size must be 16 (got %d)", fn, block_size);
+  if (head_dim != 64 && head_dim != 128)
+    return fail(NSD_ERR_UNSUPPORTED, "%s: head_dim must be 64 or 128 (got %d)", fn, head_dim);
+  if (num_kv_heads < 1 || num_q_heads < 1 || num_q_heads % num_kv_heads)
+    return fail(NSD_ERR_SHAPE, "%s: num_q_heads (%d) must be a positive multiple of "
+                "num_kv_heads (%d)", fn, num_q_heads, num_kv_heads);
+  if (total_q < 0 || max_q_per_seq < 1 || max_seq_len < 1 || max_blocks_per_seq < 1 ||
+      num_blocks < 0)
+    return fail(NSD_ERR_SHAPE, "%s: total_q, max_q_per_seq, max_seq_len, max_blocks_per_seq or "
+                "num_blocks out of range", fn);
+  if ((int64_t)total_q * num_q_heads > INT32_MAX)
+    return fail(NSD_ERR_UNSUPPORTED, "%s: more than 2^31-1 query rows", fn);
+  if (num_blocks > INT32_MAX || num_blocks * num_kv_heads > INT32_MAX)
+    return fail(NSD_ERR_UNSUPPORTED, "%s: more than 2^31-1 (block, KV head) tiles in a pool", fn);
+  if (!std::isfinite(scale)) return fail(NSD_ERR_SHAPE, "%s: scale must be finite", fn);
+  if (!(softcap >= 0.f) || std::isinf(softcap))
+    return fail(NSD_ERR_SHAPE, "%s: softcap must be finite and not negative (0: none)", fn);
+  if (bs == 0 || total_q == 0) return NSD_OK;
+  if (!q || !block_table || !seq_lens || !q_indptr || !out || (num_blocks && (!k_cache || !v_cache)))
+    return fail(NSD_ERR_NULL, "%s: NULL pointer argument", fn);
+  if (((uintptr_t)q | (uintptr_t)k_cache | (uintptr_t)v_cache | (uintptr_t)out) % 16)
+    return fail(NSD_ERR_SHAPE, "%s: q, out and the caches must be 16-byte aligned", fn);
+  const Plan pl = plan(bs, total_q, num_q_heads, num_kv_heads, max_seq_len);
+  const size_t need = workspace_bytes(pl, total_q, num_q_heads, head_dim);
+  if (need && (!workspace || workspace_size < need || (uintptr_t)workspace % 16))
+    return fail(NSD_ERR_WORKSPACE, "%s: a 16-byte aligned workspace of %zu bytes needed, %zu given",
+                fn, need, workspace ? workspace_size : (size_t)0);
+  const int64_t groups = pl.items * num_kv_heads * pl.splits;
+  if (groups > INT32_MAX) return fail(NSD_ERR_UNSUPPORTED, "%s: too many workgroups", fn);
+  Params P;
+  P.q = (const uint16_t*)q;
+  P.k = (const uint16_t*)k_cache;
+  P.v = (const uint16_t*)v_cache;
+  P.first = first_keys;
+  P.slopes = slopes;
+  P.out = (uint16_t*)out;
+  P.part = (float*)workspace;
+  P.num_blocks = num_blocks;
+  P.rows = (int64_t)total_q * num_q_heads;
+  P.scale = std::fabs(scale);
+  P.cap = softcap;
+  P.negate = std::signbit(scale) ? 0x80008000u : 0u;
+  P.width = max_blocks_per_seq;
+  P.bs = bs;
+  P.total_q = total_q;
+  P.hq = num_q_heads;
+  P.hkv = num_kv_heads;
+  P.group = num_q_heads / num_kv_heads;
+  P.max_len = num_blocks ? max_seq_len : 0;   // without a pool nothing is visible
+  P.items = (int32_t)pl.items;
+  P.splits = pl.splits;
+  clear_stale_error();
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)groups), dim3(kThreads), 0, (hipStream_t)stream, P,
+                       block_table, seq_lens, q_indptr, prefix_lens);
+  };
+  const bool cap = softcap > 0.f, bias = slopes != nullptr;
+  if (head_dim == 64) {
+    if (cap) bias ? go(chunk_kernel<64, true, true>) : go(chunk_kernel<64, true, false>);
+    else bias ? go(chunk_kernel<64, false, true>) : go(chunk_kernel<64, false, false>);
+  } else {
+    if (cap) bias ? go(chunk_kernel<128, true, true>) : go(chunk_kernel<128, true, false>);
+    else bias ? go(chunk_kernel<128, false, true>) : go(chunk_kernel<128, false, false>);
+  }
+  if (const nsd_status st = check_launch(fn)) return st;
+  if (pl.splits > 1) {
+    const int per = 1024 / head_dim;
+    const dim3 grid((uint32_t)((P.rows + per - 1) / per));
+    if (head_dim == 64)
+      hipLaunchKernelGGL(join_kernel<64>, grid, dim3(256), 0, (hipStream_t)stream, P.part, P.out,
+                         P.rows, pl.splits);
+    else
+      hipLaunchKernelGGL(join_kernel<128>, grid, dim3(256), 0, (hipStream_t)stream, P.part, P.out,
+                         P.rows, pl.splits);
+    return check_launch(fn);
+  }
+  return NSD_OK;
+}

@@ -1,0 +1,296 @@
+// Rotary positions for a step's query and key rows, and its K/V rows into
+// their slots of the paged cache.
+//
+// Pair i of a head (dimensions i and i + R/2 of the R rotated ones, or 2i and
+// 2i + 1) belongs to axis a(i) of the positions (time, height, width for
+// images) and turns by angle = pos[a(i)][row] * inv_freq[i]:
+//     (x, y) -> (x cos - y sin, x sin + y cos)
+// in fp32, rounded once to bf16.  A position of 10^6 at frequency 1 has no
+// fractional turn left in fp32 (its steps are 0.06 there), so the angle is
+// formed and reduced to a turn in fp64, once per row and pair for all heads.
+//
+// The work is memory traffic: (2 Hq + 4 Hkv) D 2 bytes a row.  A workgroup
+// takes `rows_per` consecutive rows and `heads_per` KV heads with their query
+// heads: all heads share its angles in LDS.  The cache's K plane takes a row's
+// 8 dimensions as 16 bytes with the slots adjacent, its V plane 2 bytes a row
+// with the 16 slots of a dimension adjacent, so rows that follow each other in
+// one block (a run) are written together, a whole 32-byte V sector where the
+// run fills its block.  A run is at most 16 rows; the workgroup whose rows
+// hold its first row takes all of it.  Slots that a run does not fill are not
+// touched (narrower stores), so rows may name slots in any order.
+#include "nsd_internal.h"
+
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+
+constexpr int kThreads = 256;
+constexpr int kMaxAxes = 4;
+constexpr int kRows = 16;              // rows of a workgroup, at most
+constexpr int kSpan = kRows + 15;      // with the rest of a run begun in them
+
+struct RopeArgs {
+  const uint16_t *q, *k, *v;
+  uint16_t *q_out, *k_pool, *v_pool;
+  const int32_t *pos, *slots;
+  const float* freq;
+  int64_t q_stride, k_stride, v_stride;   // elements between rows
+  int64_t num_slots;
+  int32_t cuts[kMaxAxes];                 // pairs below cuts[a] belong to axes up to a
+  int32_t total, hq, hkv, rot, rows_per, heads_per;
+};
+
+__device__ inline float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ inline float hi_f(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+// two fp32 to bf16 (nearest even), the first in the low half
+__device__ inline uint32_t pack(float a, float b) {
+  const bf16x2 v = __builtin_convertvector(f32x2{a, b}, bf16x2);
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// The first row of a run: not the slot after its predecessor's within one block.
+__device__ inline bool begins(const int32_t* slots, int64_t i) {
+  if (i == 0) return true;
+  const int32_t s = slots[i];
+  return s < 0 || s % 16 == 0 || slots[i - 1] != s - 1;
+}
+
+// Two sets of 8 dimensions turned: half layout x = dims 8c.., y = dims R/2 + 8c..
+__device__ inline void turn_half(u32x4& x, u32x4& y, const float2* cs) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 a = cs[2 * e], b = cs[2 * e + 1];
+    const float x0 = lo_f(x[e]), x1 = hi_f(x[e]), y0 = lo_f(y[e]), y1 = hi_f(y[e]);
+    x[e] = pack(x0 * a.x - y0 * a.y, x1 * b.x - y1 * b.y);
+    y[e] = pack(x0 * a.y + y0 * a.x, x1 * b.y + y1 * b.x);
+  }
+}
+// pairs of adjacent dimensions: x's pairs have angles cs[0..3], y's cs[4..7]
+__device__ inline void turn_adjacent(u32x4& x, u32x4& y, const float2* cs) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 a = cs[e], b = cs[4 + e];
+    const float x0 = lo_f(x[e]), x1 = hi_f(x[e]), y0 = lo_f(y[e]), y1 = hi_f(y[e]);
+    x[e] = pack(x0 * a.x - x1 * a.y, x0 * a.y + x1 * a.x);
+    y[e] = pack(y0 * b.x - y1 * b.y, y0 * b.y + y1 * b.x);
+  }
+}
+
+// Unit c of a head: 16 dimensions at offsets *x and *y.  The first rot/16 units are turned,
+// with the angles 8c.. of their row; the others pass.
+template <bool ADJ>
+__device__ inline bool unit(int c, int rot, int* x, int* y) {
+  const bool turned = c < rot / 16;
+  *x = !turned || ADJ ? 16 * c : 8 * c;
+  *y = !turned || ADJ ? 16 * c + 8 : rot / 2 + 8 * c;
+  return turned;
+}
+
+template <int D, bool ADJ>
+__global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeArgs A) {
+  __shared__ float2 turns[kSpan][D / 2];   // (cos, sin)
+  __shared__ int32_t slot[kSpan], first[kSpan + 1];   // rows' slots; runs' first rows
+  __shared__ int32_t span[2], runs;
+  const int tid = threadIdx.x;
+  const int64_t i0 = (int64_t)blockIdx.x * A.rows_per;
+  const int g0 = blockIdx.y * A.heads_per, gn = min(A.heads_per, A.hkv - g0);
+  // rows [begin, end): from the first run begun at or after i0 to the first begun at or
+  // after i0 + rows_per
+  if (tid < 64) {
+    const int64_t i = i0 + tid;
+    const bool b = tid < kSpan + 1 && (i >= A.total || begins(A.slots, i));
+    const uint64_t m = __ballot(b);
+    // a run is at most 16 rows, so both searches end within 16
+    const int lo = __builtin_ctzll(m), hi = A.rows_per + __builtin_ctzll(m >> A.rows_per);
+    if (tid == 0) {
+      span[0] = lo;
+      span[1] = min(hi, (int)min(A.total - i0, (int64_t)kSpan));
+    }
+    const bool mine = b && tid >= lo && tid < hi && i < A.total;
+    const uint64_t mm = __ballot(mine);
+    if (mine) first[__popcll(mm & ((1ull << tid) - 1))] = tid;
+    if (tid == 0) runs = __popcll(mm);
+    if (tid < kSpan) slot[tid] = i < A.total ? A.slots[i] : -1;
+  }
+  __syncthreads();
+  const int lo = span[0], n = span[1] - lo;   // rows i0 + lo + [0, n)
+  if (n <= 0) return;
+  const int64_t base = i0 + lo;
+  const int pairs = A.rot / 2;
+  for (int u = tid; u < n * pairs; u += kThreads) {
+    const int row = u / pairs, p = u - row * pairs;
+    int axis = 0;
+#pragma unroll
+    for (int a = 0; a < kMaxAxes - 1; ++a) axis += p >= A.cuts[a];
+    const double t = (double)A.pos[(int64_t)axis * A.total + base + row] * (double)A.freq[p] *
+                     0.15915494309189533577;   // turns
+    float s, c;
+    sincospif((float)(2.0 * (t - rint(t))), &s, &c);
+    turns[row][p] = make_float2(c, s);
+  }
+  __syncthreads();
+  const int group = A.hq / A.hkv;
+  constexpr int U = D / 16;
+  // query rows
+  const int qh = gn * group;
+  for (int u = tid; u < n * qh * U; u += kThreads) {
+    const int c = u % U, h = u / U % qh, row = u / U / qh;
+    int xo, yo;
+    const bool turned = unit<ADJ>(c, A.rot, &xo, &yo);
+    const int64_t head = (int64_t)(g0 * group + h) * D;
+    const uint16_t* src = A.q + (base + row) * A.q_stride + head;
+    u32x4 x = *(const u32x4*)(src + xo), y = *(const u32x4*)(src + yo);
+    if (turned) {
+      if (ADJ) turn_adjacent(x, y, &turns[row][8 * c]);
+      else turn_half(x, y, &turns[row][8 * c]);
+    }
+    uint16_t* dst = A.q_out + (base + row) * A.hq * D + head;
+    *(u32x4*)(dst + xo) = x;
+    *(u32x4*)(dst + yo) = y;
+  }
+  // key rows: neighbouring lanes take neighbouring rows, whose slots are adjacent in the plane
+  for (int u = tid; u < n * gn * U; u += kThreads) {
+    const int row = u % n, c = u / n % U, g = g0 + u / n / U;
+    const int64_t s = slot[lo + row];
+    if (s < 0 || s >= A.num_slots) continue;
+    int xo, yo;
+    const bool turned = unit<ADJ>(c, A.rot, &xo, &yo);
+    const uint16_t* src = A.k + (base + row) * A.k_stride + (int64_t)g * D;
+    u32x4 x = *(const u32x4*)(src + xo), y = *(const u32x4*)(src + yo);
+    if (turned) {
+      if (ADJ) turn_adjacent(x, y, &turns[row][8 * c]);
+      else turn_half(x, y, &turns[row][8 * c]);
+    }
+    uint16_t* dst = A.k_pool + (s / 16 * A.hkv + g) * (D * 16) + s % 16 * 8;
+    *(u32x4*)(dst + xo * 16) = x;
+    *(u32x4*)(dst + yo * 16) = y;
+  }
+  // value rows: two dimensions of a run
+  for (int u = tid; u < runs * gn * (D / 2); u += kThreads) {
+    const int c = u % (D / 2), g = g0 + u / (D / 2) % gn, run = u / (D / 2) / gn;
+    const int a = first[run], b = run + 1 < runs ? first[run + 1] : span[1];
+    const int64_t s = slot[a];
+    if (s < 0 || s >= A.num_slots) continue;
+    const int s0 = (int)(s % 16);
+    const uint16_t* src = A.v + (base + (a - lo)) * A.v_stride + (int64_t)g * D + 2 * c;
+    uint32_t w[16];
+#pragma unroll
+    for (int p = 0; p < 16; ++p) {
+      const int j = p - s0;
+      w[p] = j >= 0 && j < b - a ? *(const uint32_t*)(src + j * A.v_stride) : 0u;
+    }
+    uint16_t* dst = A.v_pool + ((s / 16 * A.hkv + g) * D + 2 * c) * 16;
+    if (s0 == 0 && b - a == 16) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        u32x4 even, odd;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t p = w[8 * h + 2 * e], q = w[8 * h + 2 * e + 1];
+          even[e] = (p & 0xffffu) | q << 16;
+          odd[e] = p >> 16 | (q & 0xffff0000u);
+        }
+        ((u32x4*)dst)[h] = even;
+        ((u32x4*)dst)[2 + h] = odd;
+      }
+    } else {
+#pragma unroll
+      for (int p = 0; p < 16; ++p) {
+        if (p < s0 || p >= s0 + (b - a)) continue;
+        dst[p] = (uint16_t)w[p];
+        dst[16 + p] = (uint16_t)(w[p] >> 16);
+      }
+    }
+  }
+}
+
+}  // namespace
+
+extern "C" nsd_status nsd_rope_append(void* k_pool, void* v_pool, int64_t num_blocks,
+                                      const void* q, int64_t q_stride, const void* k_new,
+                                      int64_t k_stride, const void* v_new, int64_t v_stride,
+                                      const int32_t* positions, const float* inv_freq,
+                                      const int32_t* sections, int32_t n_axes, int32_t rot_dim,
+                                      int32_t interleaved, const int32_t* slots, int32_t total_q,
+                                      int32_t num_q_heads, int32_t num_kv_heads,
+                                      int32_t block_size, int32_t head_dim, void* q_out,
+                                      void* stream) {
+  using namespace nsd;
+  const char* fn = "rope_append";
+  if (block_size != NSD_BLOCK_SIZE)
+    return fail(NSD_ERR_UNSUPPORTED, "%s: block_size must be 16 (got %d)", fn, block_size);
+  if (head_dim != 64 && head_dim != 128)
+    return fail(NSD_ERR_UNSUPPORTED, "%s: head_dim must be 64 or 128 (got %d)", fn, head_dim);
+  if (num_kv_heads < 1 || num_q_heads < 1 || num_q_heads % num_kv_heads || num_q_heads > 65535)
+    return fail(NSD_ERR_SHAPE, "%s: num_q_heads (%d) must be a positive multiple of "
+                "num_kv_heads (%d), at most 65535", fn, num_q_heads, num_kv_heads);
+  if (total_q < 0 || num_blocks < 0) return fail(NSD_ERR_SHAPE, "%s: negative size", fn);
+  if (num_blocks > (1 << 27) || num_blocks * num_kv_heads > 0x7fffffff)
+    return fail(NSD_ERR_UNSUPPORTED, "%s: more than 2^27 blocks or 2^31-1 (block, KV head) "
+                "tiles in a pool", fn);
+  if (rot_dim < 0 || rot_dim > head_dim || rot_dim % 16)
+    return fail(NSD_ERR_SHAPE, "%s: rot_dim must be a multiple of 16 in [0, head_dim] (got %d)",
+                fn, rot_dim);
+  if (n_axes < 1 || n_axes > kMaxAxes)
+    return fail(NSD_ERR_SHAPE, "%s: n_axes must be in [1, %d]", fn, kMaxAxes);
+  if (n_axes > 1 && !sections) return fail(NSD_ERR_NULL, "%s: sections is NULL", fn);
+  RopeArgs A;
+  int64_t upto = 0;
+  for (int a = 0; a < kMaxAxes; ++a) {
+    if (a < n_axes) {
+      const int32_t n = n_axes > 1 || sections ? sections[a] : rot_dim / 2;
+      if (n < 0) return fail(NSD_ERR_SHAPE, "%s: a negative section", fn);
+      upto += n;
+    }
+    A.cuts[a] = a < n_axes - 1 ? (int32_t)(upto < head_dim ? upto : head_dim) : head_dim;
+  }
+  if (upto != rot_dim / 2)
+    return fail(NSD_ERR_SHAPE, "%s: the sections must hold rot_dim / 2 = %d pairs (got %lld)", fn,
+                rot_dim / 2, (long long)upto);
+  if (total_q == 0) return NSD_OK;
+  if (!q || !k_new || !v_new || !slots || !q_out || (rot_dim && (!positions || !inv_freq)) ||
+      (num_blocks && (!k_pool || !v_pool)))
+    return fail(NSD_ERR_NULL, "%s: NULL pointer argument", fn);
+  const int64_t q_row = (int64_t)num_q_heads * head_dim, kv_row = (int64_t)num_kv_heads * head_dim;
+  const int64_t most = (int64_t)1 << 40;
+  if (q_stride < q_row || k_stride < kv_row || v_stride < kv_row || q_stride > most ||
+      k_stride > most || v_stride > most)
+    return fail(NSD_ERR_SHAPE, "%s: a row stride is shorter than its row", fn);
+  if ((q_stride | k_stride | v_stride) % 8 ||
+      ((uintptr_t)q | (uintptr_t)k_new | (uintptr_t)v_new | (uintptr_t)q_out |
+       (uintptr_t)k_pool | (uintptr_t)v_pool) % 16)
+    return fail(NSD_ERR_SHAPE, "%s: rows and planes must be 16-byte aligned", fn);
+  if (q_out == q && q_stride != q_row)
+    return fail(NSD_ERR_SHAPE, "%s: q is turned in place only where its rows are dense", fn);
+  A.q = (const uint16_t*)q;
+  A.k = (const uint16_t*)k_new;
+  A.v = (const uint16_t*)v_new;
+  A.q_out = (uint16_t*)q_out;
+  A.k_pool = (uint16_t*)k_pool;
+  A.v_pool = (uint16_t*)v_pool;
+  A.pos = positions;
+  A.slots = slots;
+  A.freq = inv_freq;
+  A.q_stride = q_stride;
+  A.k_stride = k_stride;
+  A.v_stride = v_stride;
+  A.num_slots = num_blocks * NSD_BLOCK_SIZE;
+  A.total = total_q;
+  A.hq = num_q_heads;
+  A.hkv = num_kv_heads;
+  A.rot = rot_dim;
+  A.rows_per = kRows;
+  A.heads_per = 1;
+  const dim3 grid((uint32_t)(((int64_t)total_q + A.rows_per - 1) / A.rows_per),
+                  (uint32_t)((num_kv_heads + A.heads_per - 1) / A.heads_per));
+  clear_stale_error();
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, (hipStream_t)stream, A);
+  };
+  if (head_dim == 64) interleaved ? go(rope_append_kernel<64, true>) : go(rope_append_kernel<64, false>);
+  else interleaved ? go(rope_append_kernel<128, true>) : go(rope_append_kernel<128, false>);
+  return check_launch(fn);
+}

@@ -14,6 +14,7 @@
 
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -42,6 +43,11 @@ struct Api {
   decltype(&nsd_kv_append_layers) kv_append_layers;
   decltype(&nsd_spec_accept_commit) spec_accept_commit;
   decltype(&nsd_sample_steps) sample_steps;
+  decltype(&nsd_plan_blocks) plan_blocks;
+  decltype(&nsd_trim_blocks) trim_blocks;
+  decltype(&nsd_rope_append) rope_append;
+  decltype(&nsd_chunk_attention) chunk_attention;
+  decltype(&nsd_chunk_attention_workspace_size) chunk_ws;
 } api;
 
 // Thrown (before anything is enqueued) for arguments the Python path handles.
@@ -687,6 +693,192 @@ PyObject* py_draft_stage(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // bind(addresses): the library's entry points, in the order of Api.
+// The prompt path's tensors lie on the current device, all of them (the Python path switches
+// to another device, or names the tensor that is elsewhere).
+at::Device here(const Tensor& t) {
+  need(t.device().index() == c10::hip::current_device());
+  return t.device();
+}
+
+const Tensor& typed(PyObject* o, at::ScalarType type, at::Device dev) {
+  const Tensor& t = tensor(o, type);
+  need(t.device() == dev);
+  return t;
+}
+
+// `n` int32 entries; a new tensor (kept by own) where o is None and one may be made.
+int32_t* entries(PyObject* o, int64_t n, const Tensor& like, Tensor* own = nullptr) {
+  if (own && o == Py_None) {
+    *own = at::empty({n}, like.options().dtype(at::kInt));
+    return own->data_ptr<int32_t>();
+  }
+  const Tensor& t = typed(o, at::kInt, like.device());
+  need(t.numel() == n);
+  if (own) *own = t;
+  return t.data_ptr<int32_t>();
+}
+
+template <int N>
+PyObject* wrap_list(void* t) {
+  PyObject* list = PyList_New(N);
+  for (int i = 0; list && i < N; ++i)
+    PyList_SET_ITEM(list, i, THPVariable_Wrap(((Tensor*)t)[i]));
+  return list;
+}
+
+PyObject* py_plan_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  // table, owned, lens, indptr, free, free_count, total_q, new_owned, new_lens, new_count,
+  // granted, slots
+  return entry([&]() -> PyObject* {
+    need(n == 12);
+    const Tensor &t = i32(a[0]), &f = i32(a[4]);
+    need(t.dim() == 2 && here(t) == f.device());
+    const int32_t bs = small(t.size(0)), width = small(t.size(1)), total = integer(a[6]);
+    need(total >= 0);
+    const int32_t *owned = entries(a[1], bs, t), *lens = entries(a[2], bs, t),
+                  *indptr = entries(a[3], (int64_t)bs + 1, t), *count = entries(a[5], 1, t);
+    const int32_t capacity = small(f.numel());
+    Tensor out[5];
+    int32_t *o = entries(a[7], bs, t, &out[0]), *l = entries(a[8], bs, t, &out[1]),
+            *c = entries(a[9], 1, t, &out[2]), *g = entries(a[10], bs, t, &out[3]),
+            *s = entries(a[11], total, t, &out[4]);
+    int32_t *table = t.data_ptr<int32_t>(), *ids = f.data_ptr<int32_t>();
+    void* stream = stream_of(t);
+    return unlocked([&] {
+      check("plan_blocks", api.plan_blocks(table, width, owned, lens, indptr, bs, total, ids,
+                                           capacity, count, o, l, c, g, s, stream));
+    }, wrap_list<5>, out);
+  });
+}
+
+PyObject* py_trim_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  // table, owned, keep, free, free_count, new_owned, new_count
+  return entry([&]() -> PyObject* {
+    need(n == 7);
+    const Tensor &t = i32(a[0]), &f = i32(a[3]);
+    need(t.dim() == 2 && here(t) == f.device());
+    const int32_t bs = small(t.size(0)), width = small(t.size(1)), capacity = small(f.numel());
+    const int32_t *owned = entries(a[1], bs, t), *keep = entries(a[2], bs, t),
+                  *count = entries(a[4], 1, t);
+    Tensor out[2];
+    int32_t *o = entries(a[5], bs, t, &out[0]), *c = entries(a[6], 1, t, &out[1]);
+    int32_t *table = t.data_ptr<int32_t>(), *ids = f.data_ptr<int32_t>();
+    void* stream = stream_of(t);
+    return unlocked([&] {
+      check("trim_blocks", api.trim_blocks(table, width, owned, keep, bs, ids, capacity, count, o,
+                                           c, stream));
+    }, wrap_list<2>, out);
+  });
+}
+
+// [rows][heads][D] bf16 rows, dense within a row; their stride.
+const Tensor& head_rows(PyObject* o, int64_t* stride) {
+  const Tensor& t = any_tensor(o);
+  need(t.scalar_type() == at::kBFloat16 && t.is_cuda() && t.dim() == 3);
+  const int64_t h = t.size(1), d = t.size(2);
+  need((h <= 1 || t.stride(1) == d) && (d <= 1 || t.stride(2) == 1));
+  *stride = t.size(0) > 1 ? t.stride(0) : h * d;
+  return t;
+}
+
+PyObject* py_rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  // k_pool, v_pool, q, k, v, positions, freq, slots, sections, interleaved, q_out
+  return entry([&]() -> PyObject* {
+    need(n == 11);
+    int64_t qs, ks, vs;
+    const Tensor &q = head_rows(a[2], &qs), &k = head_rows(a[3], &ks), &v = head_rows(a[4], &vs);
+    const at::Device dev = here(q);
+    const int64_t rows = q.size(0), d = q.size(2), hkv = k.size(1);
+    need(k.device() == dev && v.device() == dev && k.size(0) == rows && k.size(2) == d &&
+         v.sizes() == k.sizes());
+    const Planes pool = planes(typed(a[0], at::kBFloat16, dev), typed(a[1], at::kBFloat16, dev),
+                               false, hkv, d);
+    const Tensor &pos = typed(a[5], at::kInt, dev), &freq = typed(a[6], at::kFloat, dev);
+    need(pos.dim() == 1 || pos.dim() == 2);
+    const int64_t axes = pos.dim() == 1 ? 1 : pos.size(0);
+    need(axes >= 1 && axes <= 64 && pos.numel() == axes * rows);
+    const int32_t* slots = entries(a[7], rows, q);
+    int32_t cuts[64];
+    if (a[8] == Py_None) {
+      need(axes == 1);
+    } else {
+      const bool list = PyList_CheckExact(a[8]);
+      need(list || PyTuple_CheckExact(a[8]));
+      need((list ? PyList_GET_SIZE(a[8]) : PyTuple_GET_SIZE(a[8])) == axes);
+      for (int64_t i = 0; i < axes; ++i)
+        cuts[i] = integer(list ? PyList_GET_ITEM(a[8], i) : PyTuple_GET_ITEM(a[8], i));
+    }
+    need(PyBool_Check(a[9]));
+    const int adjacent = a[9] == Py_True;
+    Tensor out = output(a[10], at::kBFloat16, q.sizes(), q);
+    need(out.device() == dev);
+    const int32_t total = small(rows), hq = small(q.size(1)), rot = small(2 * freq.numel());
+    const int32_t* sections = a[8] == Py_None ? nullptr : cuts;
+    const char *qp = (char*)q.data_ptr(), *kp = (char*)k.data_ptr(), *vp = (char*)v.data_ptr();
+    char* op = (char*)out.data_ptr();
+    const int32_t* pp = pos.data_ptr<int32_t>();
+    const float* fp = freq.data_ptr<float>();
+    void* stream = stream_of(q);
+    return unlocked([&] {
+      check("rope_append",
+            api.rope_append(pool.k, pool.v, pool.blocks, qp, qs, kp, ks, vp, vs, pp, fp, sections,
+                            (int32_t)axes, rot, adjacent, slots, total, hq, (int32_t)hkv,
+                            NSD_BLOCK_SIZE, (int32_t)d, op, stream));
+    }, wrap, &out);
+  });
+}
+
+float number(PyObject* o) {
+  if (PyFloat_CheckExact(o)) return (float)PyFloat_AS_DOUBLE(o);
+  return (float)integer(o);
+}
+
+PyObject* py_chunk_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  // q, k, v, table, lens, indptr, max_q, max_len, scale, softcap, slopes, first_keys,
+  // prefix_lens, out, workspace
+  return entry([&]() -> PyObject* {
+    need(n == 15);
+    const Tensor &q = bf16(a[0]), &k = bf16(a[1]);
+    need(q.dim() == 3 && k.dim() == 5);
+    const at::Device dev = here(q);
+    need(k.device() == dev);
+    Batch b;
+    const int32_t total = small(q.size(0));
+    b.hq = small(q.size(1));
+    b.d = small(q.size(2));
+    b.hkv = small(k.size(1));
+    const Planes pool = planes(k, typed(a[2], at::kBFloat16, dev), false, b.hkv, b.d);
+    for (int i = 3; i < 6; ++i) typed(a[i], at::kInt, dev);
+    metadata(b, a[3], a[4], a[5], a[6], a[7]);
+    b.scale = scale_of(a[8], b.d);
+    const float cap = number(a[9]);
+    const float* slopes = nullptr;
+    if (a[10] != Py_None) {
+      const Tensor& t = typed(a[10], at::kFloat, dev);
+      need(t.numel() == b.hq);
+      slopes = t.data_ptr<float>();
+    }
+    const int32_t* first = a[11] == Py_None ? nullptr : entries(a[11], total, q);
+    const int32_t* prefix = a[12] == Py_None ? nullptr : entries(a[12], b.bs, q);
+    Tensor out = output(a[13], at::kBFloat16, q.sizes(), q), own;
+    need(out.device() == dev);
+    const size_t bytes =
+        a[14] == Py_None ? api.chunk_ws(b.bs, total, b.hq, b.hkv, b.d, b.max_q, b.max_len) : 0;
+    const Tensor& ws = workspace(a[14], q, bytes, own);
+    b.ws = (char*)ws.data_ptr();
+    b.ws_bytes = ws.numel();
+    b.stream = stream_of(q);
+    char *qp = (char*)q.data_ptr(), *op = (char*)out.data_ptr();
+    return unlocked([&] {
+      check("chunk_attention",
+            api.chunk_attention(qp, pool.k, pool.v, pool.blocks, b.table, b.width, b.lens,
+                                b.indptr, b.bs, total, b.hq, b.hkv, b.d, NSD_BLOCK_SIZE, b.max_q,
+                                b.max_len, b.scale, cap, slopes, first, prefix, op, b.ws,
+                                b.ws_bytes, b.stream));
+    }, wrap, &out);
+  });
+}
+
 PyObject* py_bind(PyObject*, PyObject* addresses) {
   void** to = (void**)&api;
   const Py_ssize_t n = sizeof(Api) / sizeof(void*);
@@ -713,6 +905,10 @@ PyMethodDef methods[] = {FAST(verify_attention),
                          FAST(kv_gather),
                          FAST(kv_append),
                          FAST(commit_lengths),
+                         FAST(plan_blocks),
+                         FAST(trim_blocks),
+                         FAST(rope_append),
+                         FAST(chunk_attention),
                          FAST(verify_round),
                          FAST(draft_stage),
                          {"bind", py_bind, METH_O, nullptr},

@@ -10,9 +10,14 @@ the pool).
 
 The draft stage that precedes it (Eq. 1) is composed the same way: K steps of
 append, single-query attention and sampling (given a workspace, the draws of
-all steps share one launch at the end where a workspace holds their sums)."""
+all steps share one launch at the end where a workspace holds their sums).
+
+The prompt path before a request's first round (prefill_chunk): blocks for the step's
+tokens, then per layer rotary positions with the rows into the cache, and attention of the
+chunk."""
 from . import (kv_gather, verify_attention, gather_verify_attention, spec_accept, kv_append,
-               commit_lengths, sample, accept_workspace_size, _native, _raised)
+               commit_lengths, sample, accept_workspace_size, plan_blocks, rope_append,
+               chunk_attention, _native, _raised)
 
 # Batches below this many requests prepare with the separate gather even when a
 # stage table is given: every pair is then moved, blocks past a request's context
@@ -175,3 +180,40 @@ def draft_stage(k_pool, v_pool, q, k_new, v_new, probs, uniforms, block_table, l
                              max_seq_len, scale=scale, out=out[i], workspace=workspace)
         sample(probs[:, i], uniforms[i], out=tokens[:, i], workspace=sample_workspace)
     return out, tokens
+
+
+def prefill_chunk(k_pool, v_pool, rows, positions, inv_freq, block_table, owned, seq_lens, q_indptr,
+                  free_blocks, free_count, total_q, max_q_per_seq, max_seq_len, sections=None,
+                  interleaved=False, out=None, workspace=None, **attention):
+    """One step of the prompt path on one stream: the next chunk of every request's prompt (or
+    its next single token) through all layers; returns (out, granted, slots).
+
+    The step's blocks and slots are planned (plan_blocks; block_table, owned, seq_lens and
+    free_count are updated in place, so that a captured step can be replayed), then per layer
+    the rows are turned and cached (rope_append) and the queries attend over the cache
+    (chunk_attention).  Pools are stacked over layers.
+
+    rows: per layer (q [total_q][Hq][D], k_new, v_new [total_q][Hkv][D]), a sequence or a
+    function of the layer's number and the previous layer's output (None before the first),
+    as a model's projections give them; positions, inv_freq, sections, interleaved: as
+    rope_append; ``attention``: chunk_attention's scale, softcap, slopes, first_keys and
+    prefix_lens.  max_seq_len bounds the lengths with the new tokens.  out:
+    [layers][total_q][Hq][D] (a list of new tensors when None); workspace as
+    chunk_attention's.
+
+    A request that is not granted its blocks (granted 0) keeps its counters and caches nothing;
+    its rows of out are to be ignored, and the caller brings its chunk again once blocks are
+    free (trim_blocks)."""
+    _, _, _, granted, slots = plan_blocks(block_table, owned, seq_lens, q_indptr, free_blocks,
+                                          free_count, total_q, new_owned=owned,
+                                          new_lens=seq_lens, new_free_count=free_count)
+    outs, o = [], None
+    for layer in range(k_pool.shape[0]):
+        q, k_new, v_new = rows(layer, o) if callable(rows) else rows[layer]
+        q = rope_append(k_pool[layer], v_pool[layer], q, k_new, v_new, positions, inv_freq, slots,
+                        sections=sections, interleaved=interleaved)
+        o = chunk_attention(q, k_pool[layer], v_pool[layer], block_table, seq_lens, q_indptr,
+                            max_q_per_seq, max_seq_len, out=None if out is None else out[layer],
+                            workspace=workspace, **attention)
+        outs.append(o)
+    return outs if out is None else out, granted, slots
