@@ -39,6 +39,7 @@ typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
 
 constexpr int kMaxBatch = 8192;
 constexpr int kWaves = 4;
@@ -109,24 +110,47 @@ template <int D>
 struct Acc {
   f32x16 o[D / 32];   // O^T: row of the wave = lane % 32, dimension 32 t + 8 (i / 4) + 4 (lane / 32) + i % 4
   float m, l;         // running maximum (log2 domain) and this lane's sum
+  bool odd;           // an infinity or NaN was left out of the product
 };
 
 // One row's mask: what its position, first key and prefix let it see.
 struct Sight {
   int p, first, prefix;
   float slope;   // log2 domain
+  int length;    // of the request
+
+  // of the block at t0, the 8 tokens this lane's operands hold: a bit for each that it sees
+  __device__ inline uint32_t sees(int t0) const {
+    uint32_t m = 0;
+    t0 += (threadIdx.x & 32) >> 2;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int t = t0 + e;
+      m |= (uint32_t)((t < prefix) | ((t <= p) & (t >= first))) << e;
+    }
+    return m;
+  }
 };
 
-// D: head dimension; CAP: capped scores; BIAS: slopes; MASK: first keys or prefixes given.
-template <int D, bool CAP, bool BIAS>
+// MFMA operands from a block's tiles.  CAP: capped scores; BIAS: slopes.
+template <int D>
 struct Tile {
   static constexpr int kHalf = D * 16;   // elements of a block's K or V tile
 
+  // This lane's K operand in its block's tile (the two halves of the lanes' 16s take a block
+  // each): its slot with bits 2 and 3 swapped.
+  static __device__ inline int key_offset() {
+    const int lane = threadIdx.x & 63, r = lane & 15;
+    return (lane >> 5) * 128 + ((r & 3) | (r & 4) << 1 | (r & 8) >> 1) * 8;
+  }
+  static __device__ inline int value_offset() {
+    const int lane = threadIdx.x & 63;
+    return (lane & 31) * 16 + (lane >> 5) * 8;
+  }
+
   // S^T of 32 tokens x 32 rows.  k: two blocks' tiles [D/8][16][8].
   static __device__ inline f32x16 scores(const uint16_t* k, const bf16x8 (&q)[D / 16]) {
-    const int lane = threadIdx.x & 63, r = lane & 15;
-    const int slot = (r & 3) | (r & 4) << 1 | (r & 8) >> 1;
-    const uint16_t* p = k + (lane >> 4 & 1) * kHalf + (lane >> 5) * 128 + slot * 8;
+    const uint16_t* p = k + (threadIdx.x >> 4 & 1) * kHalf + key_offset();
     f32x16 s = {};
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk)
@@ -136,27 +160,59 @@ struct Tile {
 
   // V^T operand of block b's dimensions 32 t ..: [D][16] as it is in the cache.
   static __device__ inline bf16x8 values(const uint16_t* v, int b, int t) {
-    const int lane = threadIdx.x & 63;
-    return *(const bf16x8*)(v + b * kHalf + (t * 32 + (lane & 31)) * 16 + (lane >> 5) * 8);
+    return *(const bf16x8*)(v + b * kHalf + t * 512 + value_offset());
   }
 };
 
-// bf16 pairs whose exponent is all ones.
-__device__ inline bool unusual(uint32_t w) {
-  return ((w & 0x7f80u) == 0x7f80u) | ((w & 0x7f800000u) == 0x7f800000u);
+// bf16 pairs: the larger of two by 16-bit halves.
+__device__ inline uint32_t max16(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a),
+                                                                __builtin_bit_cast(u16x2, b)));
+}
+// Whether any of the bf16 values of an operand is an infinity or NaN: m collects their
+// exponents.
+__device__ inline uint32_t exponents(uint32_t m, bf16x8 v) {
+  const u32x4 x = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) m = max16(m, x[e] & 0x7f807f80u);
+  return m;
+}
+__device__ inline bool unusual(uint32_t m) { return (m & 0xffffu) == 0x7f80u || m >> 16 == 0x7f80u; }
+
+// The operand's values at bits m (a bit each); the others 0.
+__device__ inline bf16x8 keep(bf16x8 v, uint32_t m) {
+  u32x4 x = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    x[e] &= (m >> (2 * e) & 1 ? 0xffffu : 0u) | (m >> (2 * e + 1) & 1 ? 0xffff0000u : 0u);
+  return __builtin_bit_cast(bf16x8, x);
 }
 
-// One stage of NSUB x 32 tokens from t0 on for a wave's rows.  hidden: some row may not see
-// some token.  valid: bit b set if block b of the stage may be read.
-template <int D, bool CAP, bool BIAS, int NSUB>
-__device__ inline void stage(Acc<D>& a, const uint16_t* k, const uint16_t* v,
-                             const bf16x8 (&q)[D / 16], const Params& P, const Sight& w, int t0,
-                             uint32_t valid, bool hidden) {
-  using T = Tile<D, CAP, BIAS>;
-  const int half = (threadIdx.x & 63) >> 5;
-  f32x16 s[NSUB];
+// A bit for each value of an operand that is +infinity (sign 0), -infinity (sign 1) or NaN.
+__device__ inline uint32_t infinite(bf16x8 v, uint32_t sign) {
+  const u32x4 x = __builtin_bit_cast(u32x4, v);
+  uint32_t m = 0;
 #pragma unroll
-  for (int u = 0; u < NSUB; ++u) s[u] = T::scores(k + u * 2 * T::kHalf, q);
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t h = x[e / 2] >> (16 * (e % 2)) & 0xffffu;
+    m |= (uint32_t)(((h & 0x7fffu) > 0x7f80u) | (h == (0x7f80u | sign << 15))) << e;
+  }
+  return m;
+}
+
+// bf16 1 at bits m, else 0.
+__device__ inline bf16x8 ones(uint32_t m) {
+  const u32x4 one = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+  return keep(__builtin_bit_cast(bf16x8, one), m);
+}
+
+// Softmax and the second product of NSUB x 32 tokens from t0 on for a wave's rows: s their
+// S^T, values(b, t) the V^T operand of block b's dimensions 32 t...  hidden: some row may not
+// see some token.  valid: bit b set if block b may be read.
+template <int D, bool CAP, bool BIAS, int NSUB, class Values>
+__device__ inline void weigh(Acc<D>& a, f32x16 (&s)[NSUB], const Values& values, const Params& P,
+                             const Sight& w, int t0, uint32_t valid, bool hidden) {
+  const int half = (threadIdx.x & 63) >> 5;
   const float c = P.scale * kLog2e;
   if constexpr (CAP || BIAS) {
     const float y = CAP ? 2.f * c / P.cap : 0.f, top = P.cap * kLog2e;
@@ -178,18 +234,15 @@ __device__ inline void stage(Acc<D>& a, const uint16_t* k, const uint16_t* v,
       }
   }
   constexpr bool kLog2 = CAP || BIAS;   // scores are in the log2 domain already
-  uint32_t seen[NSUB];                  // a bit per token of this lane
+  uint32_t seen[NSUB * 2];              // of each block, a bit per token of this lane
   if (hidden) {
 #pragma unroll
-    for (int u = 0; u < NSUB; ++u) {
-      seen[u] = 0;
+    for (int b = 0; b < NSUB * 2; ++b) {
+      seen[b] = valid >> b & 1 ? w.sees(t0 + b * 16) : 0u;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int t = t0 + u * 32 + i / 8 * 16 + half * 8 + i % 8;
-        const int block_ok = valid >> (u * 2 + i / 8) & 1;
-        const bool on = block_ok & ((t < w.prefix) | ((t <= w.p) & (t >= w.first)));
-        seen[u] |= on ? 1u << i : 0u;
-        s[u][i] = on ? s[u][i] : -INFINITY;
+      for (int e = 0; e < 8; ++e) {
+        const int i = b % 2 * 8 + e;
+        s[b / 2][i] = seen[b] >> e & 1 ? s[b / 2][i] : -INFINITY;
       }
     }
   }
@@ -221,7 +274,7 @@ __device__ inline void stage(Acc<D>& a, const uint16_t* k, const uint16_t* v,
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         e[j] = __builtin_amdgcn_exp2f(kLog2 ? s[u][i + j] - sub : fmaf(s[u][i + j], c, -sub));
-        if (hidden) e[j] = seen[u] >> (i + j) & 1 ? e[j] : 0.f;
+        if (hidden) e[j] = seen[u * 2 + i / 8] >> (i % 8 + j) & 1 ? e[j] : 0.f;
         a.l += e[j];
       }
       p[u * 2 + i / 8][i % 8 / 2] = pack(e[0], e[1]);
@@ -230,50 +283,24 @@ __device__ inline void stage(Acc<D>& a, const uint16_t* k, const uint16_t* v,
   for (int b = 0; b < NSUB * 2; ++b) {
     bf16x8 vt[D / 32];
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t) vt[t] = T::values(v, b, t);
+    for (int t = 0; t < D / 32; ++t) vt[t] = values(b, t);
     if (hidden) {
-      bool odd = false;
+      // slots past the request's last token, and blocks that may not be read, hold anything
+      const int left = w.length - (t0 + b * 16);
+      if (!(valid >> b & 1) || left < 16) {
+        const int mine = left - 8 * half;
+        const uint32_t in = !(valid >> b & 1) || mine <= 0 ? 0u : mine < 8 ? (1u << mine) - 1 : 0xffu;
 #pragma unroll
-      for (int t = 0; t < D / 32; ++t) {
-        const u32x4 x = __builtin_bit_cast(u32x4, vt[t]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) odd |= unusual(x[e]);
+        for (int t = 0; t < D / 32; ++t) vt[t] = keep(vt[t], in);
       }
-      if (__ballot(odd)) {
-        // infinities and NaN leave the product; the rows that see one get it added: the number
-        // of +infinities or NaN a row sees, and of -infinities or NaN, as products of flags
-        u32x4 flags;
+      uint32_t m = 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t bits = seen[b / 2] >> (b % 2 * 8 + 2 * e);
-          flags[e] = (bits & 1 ? 0x3f80u : 0u) | (bits & 2 ? 0x3f800000u : 0u);
-        }
+      for (int t = 0; t < D / 32; ++t) m = exponents(m, vt[t]);
+      if (__ballot(unusual(m))) {
+        a.odd = true;
 #pragma unroll
-        for (int t = 0; t < D / 32; ++t) {
-          u32x4 x = __builtin_bit_cast(u32x4, vt[t]), up, down;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            up[e] = down[e] = 0;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const uint32_t h = x[e] >> (16 * j) & 0xffffu;
-              const bool big = (h & 0x7f80u) == 0x7f80u, nan = big && (h & 0x7fu);
-              if (big && (nan || !(h & 0x8000u))) up[e] |= 0x3f80u << (16 * j);
-              if (big && (nan || (h & 0x8000u))) down[e] |= 0x3f80u << (16 * j);
-              if (big) x[e] &= ~(0xffffu << (16 * j));
-            }
-          }
-          vt[t] = __builtin_bit_cast(bf16x8, x);
-          const bf16x8 see = __builtin_bit_cast(bf16x8, flags);
-          f32x16 n = {};
-          n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, up), see, n, 0, 0, 0);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) a.o[t][i] += n[i] > 0.f ? INFINITY : 0.f;
-          n = f32x16{};
-          n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, down), see, n, 0, 0, 0);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) a.o[t][i] -= n[i] > 0.f ? INFINITY : 0.f;
-        }
+        for (int t = 0; t < D / 32; ++t)
+          vt[t] = keep(vt[t], ~(infinite(vt[t], 0) | infinite(vt[t], 1)));
       }
     }
 #pragma unroll
@@ -283,6 +310,40 @@ __device__ inline void stage(Acc<D>& a, const uint16_t* k, const uint16_t* v,
   }
 }
 
+// Adds to the rows what weigh() left out: the infinities and NaN of the V operands (v: their
+// place in this lane) of the block at t0 that each row sees.  Their numbers per row and
+// dimension are products of flags.
+template <int D>
+__device__ inline void add_infinities(Acc<D>& a, const uint16_t* v, const Sight& w, int t0) {
+  const int left = w.length - t0 - (threadIdx.x & 32) / 4;
+  const uint32_t in = left <= 0 ? 0u : left < 8 ? (1u << left) - 1 : 0xffu;
+  const bf16x8 see = ones(w.sees(t0) & in);
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t) {
+    const bf16x8 x = *(const bf16x8*)(v + t * 512);
+#pragma unroll
+    for (uint32_t sign = 0; sign < 2; ++sign) {
+      f32x16 n = {};
+      n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ones(infinite(x, sign) & in), see, n, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) a.o[t][i] += n[i] > 0.f ? (sign ? -INFINITY : INFINITY) : 0.f;
+    }
+  }
+}
+
+// weigh() from a stage's tiles in LDS.
+template <int D, bool CAP, bool BIAS, int NSUB>
+__device__ inline void stage(Acc<D>& a, const uint16_t* k, const uint16_t* v,
+                             const bf16x8 (&q)[D / 16], const Params& P, const Sight& w, int t0,
+                             uint32_t valid, bool hidden) {
+  using T = Tile<D>;
+  f32x16 s[NSUB];
+#pragma unroll
+  for (int u = 0; u < NSUB; ++u) s[u] = T::scores(k + u * 2 * T::kHalf, q);
+  weigh<D, CAP, BIAS, NSUB>(a, s, [&](int b, int t) { return T::values(v, b, t); }, P, w, t0,
+                            valid, hidden);
+}
+
 template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
     const Params P, const int32_t* __restrict__ tables, const int32_t* __restrict__ lens,
@@ -290,6 +351,8 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
   constexpr int kTile = D * 16;                     // elements of a block's K or V tile
   constexpr int kPlane = kStageBlocks * kTile;      // of a stage's K or V
   __shared__ __attribute__((aligned(16))) uint16_t buf0[2 * kPlane], buf1[2 * kPlane];
+  __shared__ float2 meet[kWaves][64];
+  using T = Tile<D>;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   // heads fastest: with 8 KV heads the workgroups of a head share an XCD's L2
   const int x = blockIdx.x, g = x % P.hkv;
@@ -308,14 +371,20 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
   const int last = L - 1;
   const int prefix = prefixes ? min(max(prefixes[r], 0), L) : 0;
 
+  // few rows: the waves share them (one or two groups of 32) and part the tokens
+  const int count = (int)min(rows - row0, (int64_t)kRows);
+  const int rgroups = count <= kWaveRows ? 1 : count <= 2 * kWaveRows ? 2 : kWaves;
+  const int rg = wave & (rgroups - 1), tgroups = kWaves / rgroups, tg = wave / rgroups;
+
   // this lane's row
-  const int64_t row = row0 + wave * kWaveRows + (lane & 31);
+  const int64_t row = row0 + rg * kWaveRows + (lane & 31);
   const bool mine = row < rows;
   const int j = mine ? (int)(row / P.group) : 0, h = mine ? (int)(row - (int64_t)j * P.group) : 0;
   Sight w;
   w.p = mine ? min(L - n + j, last) : -1;
   w.first = mine && P.first ? P.first[a0 + j] : 0;
   w.prefix = mine ? prefix : 0;
+  w.length = L;
   w.slope = BIAS && mine ? P.slopes[g * P.group + h] * kLog2e : 0.f;
   bf16x8 q[D / 16];
   {
@@ -329,29 +398,31 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
       q[kk] = __builtin_bit_cast(bf16x8, t);
     }
   }
-  // what the wave's rows, and the workgroup's, see: positions and first keys at the extremes
-  int pmin = mine ? w.p : INT32_MAX, fmax = mine ? w.first : INT32_MIN, fmin = mine ? w.first : INT32_MAX;
+  // the wave's first keys at the extremes, and its last position
+  int fmax = mine ? w.first : INT32_MIN, fmin = mine ? w.first : INT32_MAX;
 #pragma unroll
   for (int s = 1; s < 32; s *= 2) {
-    pmin = min(pmin, __shfl_xor(pmin, s));
     fmax = max(fmax, __shfl_xor(fmax, s));
     fmin = min(fmin, __shfl_xor(fmin, s));
   }
-  pmin = uniform(pmin);
   fmax = uniform(fmax);
   fmin = uniform(fmin);
-  const int64_t wave_last = min(rows, row0 + (wave + 1) * kWaveRows) - 1;
-  const int pmax = wave_last >= row0 + wave * kWaveRows
+  const int64_t wave_last = min(rows, row0 + (rg + 1) * kWaveRows) - 1;
+  const int pmax = wave_last >= row0 + rg * kWaveRows
                        ? min(L - n + (int)(wave_last / P.group), last) : -1;
-  int from = 0;   // the workgroup's first key
+  int from = 0, high = 0;   // the workgroup's first keys: the lowest and the highest
   if (P.first) {
     int32_t* at = (int32_t*)buf0;
-    if (lane == 0) at[wave] = fmin;
+    if (lane == 0) {
+      at[wave] = fmin;
+      at[kWaves + wave] = fmax;
+    }
     __syncthreads();
-    from = max(min(min(at[0], at[1]), min(at[2], at[3])), 0);
-    from = uniform(from);
+    from = uniform(max(min(min(at[0], at[1]), min(at[2], at[3])), 0));
+    high = uniform(max(max(at[4], at[5]), max(at[6], at[7])));
     __syncthreads();
   }
+  const int low = min(L - n + (int)(row0 / P.group), last);   // its first row's position
   const int to = min(L - n + (int)((min(rows, row0 + kRows) - 1) / P.group), last) + 1;   // past its last key
   // stages: those of the prefix, then from the first key's on
   const int n1 = (prefix + kStage - 1) / kStage;
@@ -366,6 +437,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
   for (int t = 0; t < D / 32; ++t) a.o[t] = f32x16{};
   a.m = -INFINITY;
   a.l = 0.f;
+  a.odd = false;
 
   const int32_t* table = tables + (int64_t)r * P.width;
   const int blocks = (L + 15) / 16;
@@ -376,7 +448,8 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
 #pragma unroll
     for (int b = 0; b < kStageBlocks; ++b) {
       const int id = table[min(t0 / 16 + b, blocks - 1)];
-      m |= (t0 / 16 + b < blocks) & (id >= 0) & (id < P.num_blocks) ? 1u << b : 0u;
+      const bool ok = (t0 / 16 + b < blocks) & (id >= 0) & (id < P.num_blocks);
+      m |= ok ? 1u << b : 0u;
     }
     return m;
   };
@@ -392,32 +465,145 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
       load_lds(P.v + at + c * 512, buf + kPlane + wave * kTile + c * 512);
     }
   };
-  auto step = [&](int i, uint16_t* now, uint16_t* next) {
-    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): this wave's part of the stage is in LDS
+  auto fetch = [&](int i, uint16_t* next) {
+    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): this wave's part of stage i is in LDS
     __syncthreads();
     if (i + 1 < i1) load(start(i + 1), next);
+  };
+  // every row of the workgroup sees every token of these stages, if their blocks are valid
+  auto open = [&](int i) {
+    const int t0 = start(i);
+    return (((t0 + kStage - 1 <= low) & (t0 >= high)) | (t0 + kStage <= prefix)) &&
+           validity(t0) == (1u << kStageBlocks) - 1;
+  };
+  auto seen_by_all = [&](int i, uint16_t* now, uint16_t* next) {
+    fetch(i, next);
+    stage<D, CAP, BIAS, 2>(a, now, now + kPlane, q, P, w, start(i), 0xf, false);
+  };
+  auto seen_by_some = [&](int i, uint16_t* now, uint16_t* next) {
+    fetch(i, next);
     const int t0 = start(i);
     const bool any = pmax >= 0 && ((t0 <= pmax && t0 + kStage > fmin) || t0 < prefix);
-    if (any) {
-      const uint32_t valid = validity(t0);
-      const bool all = valid == (1u << kStageBlocks) - 1 &&
-                       ((t0 + kStage - 1 <= pmin && t0 >= fmax) || t0 + kStage <= prefix);
-      if (all)
-        stage<D, CAP, BIAS, 2>(a, now, now + kPlane, q, P, w, t0, valid, false);
-      else
-        for (int u = 0; u < 2; ++u)
-          stage<D, CAP, BIAS, 1>(a, now + u * 2 * kTile, now + kPlane + u * 2 * kTile, q, P, w,
-                                 t0 + u * 32, valid >> (2 * u) & 3, true);
-    }
+    if (!any) return;
+    const uint32_t valid = validity(t0);
+    for (int u = 0; u < 2; ++u)
+      stage<D, CAP, BIAS, 1>(a, now + u * 2 * kTile, now + kPlane + u * 2 * kTile, q, P, w,
+                             t0 + u * 32, valid >> (2 * u) & 3, true);
   };
+  auto infinities = [&] {
+    if (!a.odd) return;   // rare: the pieces once more
+    for (int j = 2 * i0 + tg; j < 2 * i1; j += tgroups)
+      for (int b = 0; b < 2; ++b) {
+        const int t0 = start(j >> 1) + (j & 1) * 32 + b * 16;
+        const int id = table[min(t0 / 16, blocks - 1)];
+        if (t0 < L && id >= 0 && id < P.num_blocks)
+          add_infinities<D>(a, P.v + ((int64_t)id * P.hkv + g) * kTile + T::value_offset(), w, t0);
+      }
+  };
+  if (tgroups > 1) {
+    // Few rows: bound by the bytes in flight.  Every wave streams its own 32-token pieces from
+    // memory into registers, without a barrier: K of the next piece is requested once the
+    // scores have consumed this one's, V once the second product has.
+    const int j1 = 2 * i1;
+    bf16x8 kr[D / 16], vr[2][D / 32];
+    const int own = lane >> 4 & 1;   // this lane's block of the piece
+    int id[2];
+    uint32_t valid = 0;
+    auto place = [&](int j) { return start(j >> 1) + (j & 1) * 32; };
+    auto find = [&](int j) {
+      valid = 0;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int blk = place(j) / 16 + b;
+        id[b] = table[min(blk, blocks - 1)];
+        const bool ok = (blk < blocks) & (id[b] >= 0) & (id[b] < P.num_blocks);
+        valid |= ok ? 1u << b : 0u;
+        id[b] = ok ? id[b] : 0;
+      }
+    };
+    auto keys = [&] {
+      const uint16_t* p = P.k + ((int64_t)(own ? id[1] : id[0]) * P.hkv + g) * kTile + T::key_offset();
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk)
+        kr[kk] = __builtin_nontemporal_load((const bf16x8*)(p + kk * 256));
+    };
+    auto values = [&] {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const uint16_t* p = P.v + ((int64_t)id[b] * P.hkv + g) * kTile + T::value_offset();
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+          vr[b][t] = __builtin_nontemporal_load((const bf16x8*)(p + t * 512));
+      }
+    };
+    int j = 2 * i0 + tg;
+    if (j < j1) {
+      find(j);
+      keys();
+      values();
+    }
+    while (j < j1) {
+      const int t0 = place(j), next = j + tgroups;
+      const uint32_t ok = valid;
+      f32x16 s[1] = {};
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk)
+        s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kr[kk], q[kk], s[0], 0, 0, 0);
+      if (next < j1) {
+        find(next);
+        keys();
+      }
+      weigh<D, CAP, BIAS, 1>(a, s, [&](int b, int t) { return vr[b][t]; }, P, w, t0, ok, true);
+      if (next < j1) values();
+      j = next;
+    }
+    infinities();
+    // the token groups' results meet in LDS
+    a.l += other_half(a.l);
+    auto region = [&](int v) { return (float*)((v & 2 ? buf1 : buf0) + (v & 1) * kPlane) + lane; };
+    if (tg) {
+      float* to = region(wave);
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) to[(t * 16 + i) * 64] = a.o[t][i];
+      meet[wave][lane] = make_float2(a.m, a.l);
+    }
+    __syncthreads();
+    if (tg) return;
+    for (int o = 1; o < tgroups; ++o) {
+      const float2 y = meet[o * rgroups + rg][lane];
+      const float* from = region(o * rgroups + rg);
+      const float m = fmaxf(a.m, y.x);
+      const float f = a.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(a.m - m);
+      const float e = y.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(y.x - m);
+      a.m = m;
+      a.l = a.l * f + y.y * e;
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) a.o[t][i] = a.o[t][i] * f + from[(t * 16 + i) * 64] * e;
+    }
+  } else {
   if (i0 < i1) load(start(i0), buf0);
-  for (int i = i0; i < i1; i += 2) {
-    step(i, buf0, buf1);
-    if (i + 1 < i1) step(i + 1, buf1, buf0);
+  for (int i = i0; i < i1;) {
+    // the hot loop, in pairs of stages (each buffer's code apart)
+    while (i + 1 < i1 && open(i) && open(i + 1)) {
+      seen_by_all(i, buf0, buf1);
+      seen_by_all(i + 1, buf1, buf0);
+      i += 2;
+    }
+    if (i >= i1) break;
+    seen_by_some(i, buf0, buf1);
+    if (i + 1 < i1) seen_by_some(i + 1, buf1, buf0);
+    i += 2;
+  }
+  infinities();
+  a.l += other_half(a.l);
   }
 
   if (!mine) return;
-  const float l = a.l + other_half(a.l);
+  const float l = a.l;
   const float f = l == 0.f ? 0.f : 1.f / l;   // no visible token: 0
   const int64_t out_row = (int64_t)(a0 + j) * P.hq + g * P.group + h;
   if (P.splits == 1) {
