@@ -633,29 +633,63 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
   }
 }
 
-// The splits of each row joined: D/4 threads a row.
+// The splits of each row joined: D/4 threads take a row's columns, `teams` such teams (a power
+// of two) part its splits and meet in LDS.
 template <int D>
-__global__ __launch_bounds__(256) void join_kernel(const float* part, uint16_t* out, int64_t rows,
-                                                   int splits) {
-  const int64_t row = (int64_t)blockIdx.x * (1024 / D) + threadIdx.x / (D / 4);
-  const int c = threadIdx.x % (D / 4);
-  if (row >= rows) return;
+__global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ part, uint16_t* out,
+                                                   int64_t rows, int splits, int teams) {
+  constexpr int kTeam = D / 4, kTeams = 256 / kTeam;
+  __shared__ float4 sums[kTeams][kTeam];
+  __shared__ float2 meet[kTeams];   // (max, sum)
+  const int team = threadIdx.x / kTeam, c = threadIdx.x % kTeam, first = team & (teams - 1);
+  const int64_t row = (int64_t)blockIdx.x * (kTeams / teams) + team / teams;
+  const bool in = row < rows;
   const float2* ml = (const float2*)(part + (int64_t)splits * rows * D);
-  float m = -INFINITY;
-  for (int s = 0; s < splits; ++s) m = fmaxf(m, ml[s * rows + row].x);
-  float sum = 0.f;
+  float m = -INFINITY, sum = 0.f;
   float4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < splits; ++s) {
-    const float2 x = ml[s * rows + row];
-    if (x.y == 0.f) continue;   // this split saw nothing
-    const float f = __builtin_amdgcn_exp2f(x.x - m) * x.y;
-    const float4 y = *(const float4*)(part + (s * rows + row) * D + c * 4);
-    sum += f;
-    o.x += f * y.x;
-    o.y += f * y.y;
-    o.z += f * y.z;
-    o.w += f * y.w;
+  for (int s0 = first; in && s0 < splits; s0 += 4 * teams) {
+    float2 x[4];
+    float4 y[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {   // the four loads in flight; past the last split: nothing seen
+      const int s = min(s0 + u * teams, splits - 1);
+      x[u] = ml[s * rows + row];
+      y[u] = *(const float4*)(part + (s * rows + row) * D + c * 4);
+      if (s0 + u * teams >= splits || x[u].y == 0.f) x[u] = make_float2(-INFINITY, 0.f);
+    }
+    const float top = fmaxf(fmaxf(m, fmaxf(x[0].x, x[1].x)), fmaxf(x[2].x, x[3].x));
+    const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+    m = top;
+    sum *= keep;
+    o.x *= keep, o.y *= keep, o.z *= keep, o.w *= keep;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (x[u].y == 0.f) continue;
+      const float f = __builtin_amdgcn_exp2f(x[u].x - m) * x[u].y;
+      sum += f;
+      o.x += f * y[u].x, o.y += f * y[u].y, o.z += f * y[u].z, o.w += f * y[u].w;
+    }
   }
+  if (teams > 1) {
+    sums[team][c] = o;
+    if (c == 0) meet[team] = make_float2(m, sum);
+    __syncthreads();
+    if (first) return;
+    float top = m;
+    for (int t = 1; t < teams; ++t) top = fmaxf(top, meet[team + t].x);
+    const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+    sum *= keep;
+    o.x *= keep, o.y *= keep, o.z *= keep, o.w *= keep;
+    for (int t = 1; t < teams; ++t) {
+      const float2 x = meet[team + t];
+      if (x.x == -INFINITY) continue;
+      const float f = __builtin_amdgcn_exp2f(x.x - top);
+      const float4 y = sums[team + t][c];
+      sum += f * x.y;
+      o.x += f * y.x, o.y += f * y.y, o.z += f * y.z, o.w += f * y.w;
+    }
+  }
+  if (!in) return;
   const float f = sum == 0.f ? 0.f : 1.f / sum;
   u32x2 y;
   y[0] = pack(o.x * f, o.y * f);
@@ -781,14 +815,16 @@ extern "C" nsd_status nsd_chunk_attention(
   }
   if (const nsd_status st = check_launch(fn)) return st;
   if (pl.splits > 1) {
-    const int per = 1024 / head_dim;
+    const int most = 1024 / head_dim;
+    int teams = 1;
+    while (teams < most && teams * 4 < pl.splits) teams *= 2;
+    const int per = most / teams;
     const dim3 grid((uint32_t)((P.rows + per - 1) / per));
-    if (head_dim == 64)
-      hipLaunchKernelGGL(join_kernel<64>, grid, dim3(256), 0, (hipStream_t)stream, P.part, P.out,
-                         P.rows, pl.splits);
-    else
-      hipLaunchKernelGGL(join_kernel<128>, grid, dim3(256), 0, (hipStream_t)stream, P.part, P.out,
-                         P.rows, pl.splits);
+    auto join = [&](auto kernel) {
+      hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, P.part, P.out, P.rows,
+                         pl.splits, teams);
+    };
+    head_dim == 64 ? join(join_kernel<64>) : join(join_kernel<128>);
     return check_launch(fn);
   }
   return NSD_OK;
