@@ -60,7 +60,7 @@ struct Params {
   float* part;        // [splits][rows][D] normalised partial rows, then [splits][rows][2] (max, sum)
   int64_t num_blocks;
   int64_t rows;       // total_q * hq
-  float scale, cap;   // scale >= 0 (a negative one is in `negate`)
+  float scale, cap;   // scale log2 e > 0 (a negative scale's sign is in `negate`)
   uint32_t negate;    // 0x80008000: Q's signs are flipped
   int32_t width, bs, total_q, hq, hkv, group, max_len, items, splits;
 };
@@ -100,10 +100,12 @@ __device__ inline int find_request(const Params& P, const int32_t* indptr, int i
   return uniform(lo);
 }
 
-// 16 bytes a lane from `src` (its own address) to 1 KiB at `dst`, a lane's at lane * 16.
-__device__ inline void load_lds(const void* src, void* dst) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)src,
-                                   (__attribute__((address_space(3))) uint32_t*)dst, 16, 0, 0);
+// 1 KiB from src + OFFSET to dst + OFFSET, 16 bytes a lane.
+template <int OFFSET>
+__device__ inline void load_lds(const uint16_t* src, void* dst) {
+  __builtin_amdgcn_global_load_lds(
+      (const __attribute__((address_space(1))) uint32_t*)(src + (threadIdx.x & 63) * 8),
+      (__attribute__((address_space(3))) uint32_t*)dst, 16, OFFSET, 0);
 }
 
 template <int D>
@@ -121,15 +123,11 @@ struct Sight {
 
   // of the block at t0, the 8 tokens this lane's operands hold: a bit for each that it sees
   __device__ inline uint32_t sees(int t0) const {
-    uint32_t m = 0;
     t0 += (threadIdx.x & 32) >> 2;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int t = t0 + e;
-      m |= (uint32_t)((t < prefix) | ((t <= p) & (t >= first))) << e;
-    }
-    return m;
+    return (below(p - t0 + 1) & ~below(first - t0)) | below(prefix - t0);
   }
+  // the lowest n bits of 8
+  static __device__ inline uint32_t below(int n) { return (1u << min(max(n, 0), 8)) - 1; }
 };
 
 // MFMA operands from a block's tiles.  CAP: capped scores; BIAS: slopes.
@@ -206,6 +204,43 @@ __device__ inline bf16x8 ones(uint32_t m) {
   return keep(__builtin_bit_cast(bf16x8, one), m);
 }
 
+// Scores of NSUB x 32 tokens from t0 on, capped and biased, to the log2 domain (c: scale log2 e).
+template <bool CAP, bool BIAS, int NSUB>
+__device__ inline void to_log2(f32x16 (&s)[NSUB], float c, float cap, const Sight& w, int t0,
+                               int half) {
+  const float y = CAP ? 2.f * c / cap : 0.f, top = cap * kLog2e;
+  const float d0 = (float)(w.p - t0 - 8 * half);
+#pragma unroll
+  for (int u = 0; u < NSUB; ++u)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float x;
+      if constexpr (CAP) {
+        // cap tanh(x / cap): 1 - 2 / (1 + e^(2 x / cap))
+        const float e = __builtin_amdgcn_exp2f(s[u][i] * y);
+        x = fmaf(-2.f * top, __builtin_amdgcn_rcpf(1.f + e), top);
+      } else {
+        x = s[u][i] * c;
+      }
+      if constexpr (BIAS) x = fmaf(-w.slope, fabsf(d0 - (float)(u * 32 + i / 8 * 16 + i % 8)), x);
+      s[u][i] = x;
+    }
+}
+
+// The running maximum takes `top` in, where some row's grew by more than kSlack.
+template <int D>
+__device__ inline void grow(Acc<D>& a, float top) {
+  if (!__ballot(top > a.m + kSlack || a.m == -INFINITY)) return;
+  const float m = fmaxf(a.m, top);
+  const float f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(a.m - m);
+  a.m = m;
+  a.l *= f;
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) a.o[t][i] *= f;
+}
+
 // Softmax and the second product of NSUB x 32 tokens from t0 on for a wave's rows: s their
 // S^T, values(b, t) the V^T operand of block b's dimensions 32 t...  hidden: some row may not
 // see some token.  valid: bit b set if block b may be read.
@@ -213,36 +248,18 @@ template <int D, bool CAP, bool BIAS, int NSUB, class Values>
 __device__ inline void weigh(Acc<D>& a, f32x16 (&s)[NSUB], const Values& values, const Params& P,
                              const Sight& w, int t0, uint32_t valid, bool hidden) {
   const int half = (threadIdx.x & 63) >> 5;
-  const float c = P.scale * kLog2e;
-  if constexpr (CAP || BIAS) {
-    const float y = CAP ? 2.f * c / P.cap : 0.f, top = P.cap * kLog2e;
-    const float d0 = (float)(w.p - t0 - 8 * half);
-#pragma unroll
-    for (int u = 0; u < NSUB; ++u)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float x;
-        if constexpr (CAP) {
-          // cap tanh(x / cap): 1 - 2 / (1 + e^(2 x / cap))
-          const float e = __builtin_amdgcn_exp2f(s[u][i] * y);
-          x = fmaf(-2.f * top, __builtin_amdgcn_rcpf(1.f + e), top);
-        } else {
-          x = s[u][i] * c;
-        }
-        if constexpr (BIAS) x = fmaf(-w.slope, fabsf(d0 - (float)(u * 32 + i / 8 * 16 + i % 8)), x);
-        s[u][i] = x;
-      }
-  }
+  const float c = P.scale;
+  if constexpr (CAP || BIAS) to_log2<CAP, BIAS, NSUB>(s, c, P.cap, w, t0, half);
   constexpr bool kLog2 = CAP || BIAS;   // scores are in the log2 domain already
-  uint32_t seen[NSUB * 2];              // of each block, a bit per token of this lane
   if (hidden) {
 #pragma unroll
     for (int b = 0; b < NSUB * 2; ++b) {
-      seen[b] = valid >> b & 1 ? w.sees(t0 + b * 16) : 0u;
+      const uint32_t seen = valid >> b & 1 ? w.sees(t0 + b * 16) : 0u;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int i = b % 2 * 8 + e;
-        s[b / 2][i] = seen[b] >> e & 1 ? s[b / 2][i] : -INFINITY;
+        const uint32_t on = (uint32_t)((int32_t)(seen << (31 - e)) >> 31);
+        s[b / 2][i] = __uint_as_float((__float_as_uint(s[b / 2][i]) & on) | (0xff800000u & ~on));
       }
     }
   }
@@ -253,17 +270,7 @@ __device__ inline void weigh(Acc<D>& a, f32x16 (&s)[NSUB], const Values& values,
     for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
   top = fmaxf(top, other_half(top));
   if constexpr (!kLog2) top *= c;
-  if (c == 0.f && !kLog2) top = top == top ? top : -INFINITY;   // 0 times a hidden -inf
-  if (__ballot(top > a.m + kSlack || a.m == -INFINITY)) {
-    const float m = fmaxf(a.m, top);
-    const float f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(a.m - m);
-    a.m = m;
-    a.l *= f;
-#pragma unroll
-    for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) a.o[t][i] *= f;
-  }
+  grow(a, top);
   const float sub = a.m == -INFINITY ? 0.f : a.m;
   u32x4 p[NSUB * 2];
 #pragma unroll
@@ -274,7 +281,6 @@ __device__ inline void weigh(Acc<D>& a, f32x16 (&s)[NSUB], const Values& values,
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         e[j] = __builtin_amdgcn_exp2f(kLog2 ? s[u][i + j] - sub : fmaf(s[u][i + j], c, -sub));
-        if (hidden) e[j] = seen[u * 2 + i / 8] >> (i % 8 + j) & 1 ? e[j] : 0.f;
         a.l += e[j];
       }
       p[u * 2 + i / 8][i % 8 / 2] = pack(e[0], e[1]);
@@ -344,6 +350,86 @@ __device__ inline void stage(Acc<D>& a, const uint16_t* k, const uint16_t* v,
                             valid, hidden);
 }
 
+// stage() of 64 tokens that every row sees: the hot one.  Left to itself the compiler has two
+// LDS reads in flight and waits for them before every other MFMA, so the order is given:
+// eight K operands ahead of the first MFMA, the first V operands under the last ones, the
+// weights of a block under the MFMAs of the one before.
+template <int D>
+__device__ inline void open_stage(Acc<D>& a, const uint16_t* k, const uint16_t* v,
+                                  const bf16x8 (&q)[D / 16], float c) {
+  using T = Tile<D>;
+  constexpr int KK = D / 16, VT = D / 32;
+  const uint16_t* kp = k + (threadIdx.x >> 4 & 1) * T::kHalf + T::key_offset();
+  bf16x8 kf[2][KK], vf[4][VT];
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) kf[u][kk] = *(const bf16x8*)(kp + u * 2 * T::kHalf + kk * 256);
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int t = 0; t < VT; ++t) vf[b][t] = T::values(v, b, t);
+  f32x16 s[2] = {};
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+      s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[u][kk], q[kk], s[u], 0, 0, 0);
+  float top = s[0][0];
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[u][i]);
+  __builtin_amdgcn_sched_group_barrier(0x100, KK, 0);
+#pragma unroll
+  for (int i = 0; i < KK; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+  }
+#pragma unroll
+  for (int i = 0; i < KK; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, 1, 0);
+  }
+  top = fmaxf(top, other_half(top));
+  grow(a, top * c);
+  const float sub = a.m == -INFINITY ? 0.f : a.m;
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    u32x4 p;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      float e[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float x = s[b / 2][b % 2 * 8 + i + j];
+        e[j] = __builtin_amdgcn_exp2f(fmaf(x, c, -sub));
+        a.l += e[j];
+      }
+      p[i / 2] = pack(e[0], e[1]);
+    }
+    if (b < 2) {
+#pragma unroll
+      for (int t = 0; t < VT; ++t) vf[b + 2][t] = T::values(v, b + 2, t);
+    }
+#pragma unroll
+    for (int t = 0; t < VT; ++t)
+      a.o[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[b][t], __builtin_bit_cast(bf16x8, p),
+                                                       a.o[t], 0, 0, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x002, 28, 1);
+#pragma unroll
+  for (int b = 0; b < 3; ++b)
+#pragma unroll
+    for (int t = 0; t < VT; ++t) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+      if (b < 2) __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+      __builtin_amdgcn_sched_group_barrier(0x002, 28 / VT, 1);
+    }
+  __builtin_amdgcn_sched_group_barrier(0x008, VT, 1);
+}
+
 template <int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
     const Params P, const int32_t* __restrict__ tables, const int32_t* __restrict__ lens,
@@ -382,7 +468,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
   const int j = mine ? (int)(row / P.group) : 0, h = mine ? (int)(row - (int64_t)j * P.group) : 0;
   Sight w;
   w.p = mine ? min(L - n + j, last) : -1;
-  w.first = mine && P.first ? P.first[a0 + j] : 0;
+  w.first = mine && P.first ? max(P.first[a0 + j], 0) : 0;
   w.prefix = mine ? prefix : 0;
   w.length = L;
   w.slope = BIAS && mine ? P.slopes[g * P.group + h] * kLog2e : 0.f;
@@ -408,6 +494,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
   fmax = uniform(fmax);
   fmin = uniform(fmin);
   const int64_t wave_last = min(rows, row0 + (rg + 1) * kWaveRows) - 1;
+  const int pmin = min(L - n + (int)((row0 + rg * kWaveRows) / P.group), last);
   const int pmax = wave_last >= row0 + rg * kWaveRows
                        ? min(L - n + (int)(wave_last / P.group), last) : -1;
   int from = 0, high = 0;   // the workgroup's first keys: the lowest and the highest
@@ -442,53 +529,66 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
   const int32_t* table = tables + (int64_t)r * P.width;
   const int blocks = (L + 15) / 16;
   auto start = [&](int i) { return (i < n1 ? i : i - n1 + s2) * kStage; };
-  // which blocks of a stage may be read
-  auto validity = [&](int t0) {
-    uint32_t m = 0;
-#pragma unroll
-    for (int b = 0; b < kStageBlocks; ++b) {
-      const int id = table[min(t0 / 16 + b, blocks - 1)];
-      const bool ok = (t0 / 16 + b < blocks) & (id >= 0) & (id < P.num_blocks);
-      m |= ok ? 1u << b : 0u;
+  // The ids of 64 blocks (16 stages), a lane each, and of the 64 after them: a scalar load and
+  // its wait per stage would cost every stage its latency.
+  int chunk = -2, now = 0, ahead = 0;
+  uint64_t good = 0;   // which of them may be read
+  auto ids = [&](int c) { return table[min(c * 64 + lane, blocks - 1)]; };
+  auto seek = [&](int t0) {   // ids for the stage at t0; which of its blocks may be read
+    const int c = t0 >> 10;
+    if (c != chunk) {
+      now = c == chunk + 1 ? ahead : ids(c);
+      ahead = ids(c + 1);
+      good = __ballot((now >= 0) & (now < P.num_blocks) & (c * 64 + lane < blocks));
+      chunk = c;
     }
-    return m;
+    return (uint32_t)(good >> (t0 >> 4 & 63)) & ((1u << kStageBlocks) - 1);
   };
-  // wave w loads block w of the stage; an invalid one's place gets block 0
-  auto load = [&](int t0, uint16_t* buf) {
-    const int b = min(t0 / 16 + wave, blocks - 1);
-    int id = table[b];
-    id = id >= 0 && id < P.num_blocks ? id : 0;
-    const int64_t at = ((int64_t)id * P.hkv + g) * kTile + lane * 8;
-#pragma unroll
-    for (int c = 0; c < kTile / 512; ++c) {
-      load_lds(P.k + at + c * 512, buf + wave * kTile + c * 512);
-      load_lds(P.v + at + c * 512, buf + kPlane + wave * kTile + c * 512);
+  // wave w loads block w of the stage sought; an unreadable one's place gets block 0
+  auto load = [&](int t0, uint32_t valid, uint16_t* buf) {
+    const int id = valid >> wave & 1 ? __builtin_amdgcn_readlane(now, (t0 >> 4 & 63) + wave) : 0;
+    const int64_t at = ((int64_t)id * P.hkv + g) * kTile;
+    uint16_t *kd = buf + wave * kTile, *vd = kd + kPlane;
+    load_lds<0>(P.k + at, kd);
+    load_lds<1024>(P.k + at, kd);
+    if constexpr (D == 128) {
+      load_lds<2048>(P.k + at, kd);
+      load_lds<3072>(P.k + at, kd);
+    }
+    load_lds<0>(P.v + at, vd);
+    load_lds<1024>(P.v + at, vd);
+    if constexpr (D == 128) {
+      load_lds<2048>(P.v + at, vd);
+      load_lds<3072>(P.v + at, vd);
     }
   };
-  auto fetch = [&](int i, uint16_t* next) {
-    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): this wave's part of stage i is in LDS
+  auto arrived = [&] {
+    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): this wave's part of the stage is in LDS
     __syncthreads();
-    if (i + 1 < i1) load(start(i + 1), next);
   };
-  // every row of the workgroup sees every token of these stages, if their blocks are valid
-  auto open = [&](int i) {
+  // every row of the workgroup sees every token of such a stage
+  auto open = [&](int i, uint32_t valid) {
     const int t0 = start(i);
-    return (((t0 + kStage - 1 <= low) & (t0 >= high)) | (t0 + kStage <= prefix)) &&
-           validity(t0) == (1u << kStageBlocks) - 1;
+    return (((t0 + kStage - 1 <= low) & (t0 >= high)) | (t0 + kStage <= prefix)) &
+           (valid == (1u << kStageBlocks) - 1);
   };
-  auto seen_by_all = [&](int i, uint16_t* now, uint16_t* next) {
-    fetch(i, next);
-    stage<D, CAP, BIAS, 2>(a, now, now + kPlane, q, P, w, start(i), 0xf, false);
+  auto seen_by_all = [&](int i, const uint16_t* buf) {
+    if constexpr (CAP || BIAS)
+      stage<D, CAP, BIAS, 2>(a, buf, buf + kPlane, q, P, w, start(i), 0xf, false);
+    else
+      open_stage<D>(a, buf, buf + kPlane, q, P.scale);
   };
-  auto seen_by_some = [&](int i, uint16_t* now, uint16_t* next) {
-    fetch(i, next);
+  auto seen_by_some = [&](int i, uint32_t valid, const uint16_t* buf) {
     const int t0 = start(i);
-    const bool any = pmax >= 0 && ((t0 <= pmax && t0 + kStage > fmin) || t0 < prefix);
-    if (!any) return;
-    const uint32_t valid = validity(t0);
-    for (int u = 0; u < 2; ++u)
-      stage<D, CAP, BIAS, 1>(a, now + u * 2 * kTile, now + kPlane + u * 2 * kTile, q, P, w,
-                             t0 + u * 32, valid >> (2 * u) & 3, true);
+    if (pmax < 0) return;
+    for (int u = 0; u < 2; ++u) {
+      const int t = t0 + u * 32;
+      const uint32_t ok = valid >> (2 * u) & 3;
+      if (((t > pmax) | (t + 32 <= fmin)) & (t >= prefix)) continue;
+      const bool all = ((t + 31 <= pmin) & (t >= fmax)) | (t + 32 <= prefix);
+      stage<D, CAP, BIAS, 1>(a, buf + u * 2 * kTile, buf + kPlane + u * 2 * kTile, q, P, w, t, ok,
+                             !(all & (ok == 3)));
+    }
   };
   auto infinities = [&] {
     if (!a.odd) return;   // rare: the pieces once more
@@ -585,21 +685,38 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
         for (int i = 0; i < 16; ++i) a.o[t][i] = a.o[t][i] * f + from[(t * 16 + i) * 64] * e;
     }
   } else {
-  if (i0 < i1) load(start(i0), buf0);
-  for (int i = i0; i < i1;) {
-    // the hot loop, in pairs of stages (each buffer's code apart)
-    while (i + 1 < i1 && open(i) && open(i + 1)) {
-      seen_by_all(i, buf0, buf1);
-      seen_by_all(i + 1, buf1, buf0);
-      i += 2;
+    // Stages in pairs, a buffer each.  va, vb: which blocks of a pair's stages may be read.
+    uint32_t va = 0, vb = 0;
+    auto first = [&](int i) {   // stage i goes to buf0
+      if (i >= i1) return;
+      va = seek(start(i));
+      load(start(i), va, buf0);
+    };
+    first(i0);
+    for (int i = i0; i < i1; i += 2) {
+      while (i + 1 < i1) {   // the hot loop
+        vb = seek(start(i + 1));
+        if (!(open(i, va) & open(i + 1, vb)) | (pmax < 0)) break;
+        arrived();
+        load(start(i + 1), vb, buf1);
+        seen_by_all(i, buf0);
+        arrived();
+        first(i + 2);
+        seen_by_all(i + 1, buf1);
+        i += 2;
+      }
+      if (i >= i1) break;
+      arrived();
+      const uint32_t ok = va;
+      if (i + 1 < i1) load(start(i + 1), vb, buf1);
+      seen_by_some(i, ok, buf0);
+      if (i + 1 >= i1) break;
+      arrived();
+      first(i + 2);
+      seen_by_some(i + 1, vb, buf1);
     }
-    if (i >= i1) break;
-    seen_by_some(i, buf0, buf1);
-    if (i + 1 < i1) seen_by_some(i + 1, buf1, buf0);
-    i += 2;
-  }
-  infinities();
-  a.l += other_half(a.l);
+    infinities();
+    a.l += other_half(a.l);
   }
 
   if (!mine) return;
@@ -788,7 +905,8 @@ extern "C" nsd_status nsd_chunk_attention(
   P.part = (float*)workspace;
   P.num_blocks = num_blocks;
   P.rows = (int64_t)total_q * num_q_heads;
-  P.scale = std::fabs(scale);
+  // 0 becomes a factor too small to move a weight, as 0 times a hidden token's -infinity is NaN
+  P.scale = std::max(std::fabs(scale) * kLog2e, 1e-37f);
   P.cap = softcap;
   P.negate = std::signbit(scale) ? 0x80008000u : 0u;
   P.width = max_blocks_per_seq;
