@@ -30,6 +30,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace {
 
@@ -50,6 +51,11 @@ constexpr int kStage = 64;                   // tokens of a stage
 constexpr int kStageBlocks = kStage / NSD_BLOCK_SIZE;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kSlack = 8.f;                // log2 of the weights' bound
+constexpr int kSlots = 512;                  // workgroups resident on 256 CUs, two each
+constexpr int kPerLane = 4;                  // requests a lane looks at where the batch is parted
+constexpr int kPartedBatch = 64 * kPerLane;
+constexpr int kMaxSplits = 64;
+constexpr int kJoinThreads = 1024;
 
 struct Params {
   const uint16_t* q;
@@ -57,12 +63,17 @@ struct Params {
   const int32_t* first;
   const float* slopes;
   uint16_t* out;
-  float* part;        // [splits][rows][D] normalised partial rows, then [splits][rows][2] (max, sum)
+  // Split items: how many a KV head has, a record of each (splits | first place << 8, first
+  // query token, first row, rows); and by place, one a part, the rows' (max, sum) and
+  // normalised values.
+  int32_t* split_items;
+  int4* records;      // [split items][hkv]
+  float2* part_ml;    // [places][hkv][kRows]
+  float* part;        // [places][hkv][kRows][D]
   int64_t num_blocks;
-  int64_t rows;       // total_q * hq
   float scale, cap;   // scale log2 e > 0 (a negative scale's sign is in `negate`)
   uint32_t negate;    // 0x80008000: Q's signs are flipped
-  int32_t width, bs, total_q, hq, hkv, group, max_len, items, splits;
+  int32_t width, bs, total_q, hq, hkv, group, max_len, items, max_places, parted;
 };
 
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -98,6 +109,131 @@ __device__ inline int find_request(const Params& P, const int32_t* indptr, int i
     lo += last * step;
   }
   return uniform(lo);
+}
+
+// Sums and maxima over the wave's lanes up to each.
+template <class T, class Op>
+__device__ inline T wave_scan(T x, T none, Op op) {
+  auto step = [&](auto ctrl, auto rows) {
+    const int y = __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none),
+                                              __builtin_bit_cast(int, x), decltype(ctrl)::value,
+                                              decltype(rows)::value, 0xf, false);
+    x = op(x, __builtin_bit_cast(T, y));
+  };
+  using std::integral_constant;
+  const integral_constant<int, 0xf> all{};
+  step(integral_constant<int, 0x111>{}, all);   // from 1, 2, 4 and 8 lanes below in a row of 16
+  step(integral_constant<int, 0x112>{}, all);
+  step(integral_constant<int, 0x114>{}, all);
+  step(integral_constant<int, 0x118>{}, all);
+  step(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});   // the row below's last
+  step(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});   // the lower half's last
+  return x;
+}
+template <class T>
+__device__ inline T last_lane(T x) {
+  return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+__device__ inline int sum_scan(int x) { return wave_scan(x, 0, [](int a, int b) { return a + b; }); }
+
+// What a workgroup does for its KV head: split `split` of `splits` of a request's tile of rows;
+// place: of its partial result; record: of its item.  r < 0: nothing.
+struct Piece {
+  int r, tile, split, splits, place, record;
+};
+
+// The idx-th piece of a batch of at most kPartedBatch requests, found by every wave from the
+// batch's lengths (a lane has up to four requests), so that no launch and no list goes before.
+//
+// A tile's cost is the stages its request's tokens span.  A slot's fair share of the batch is
+// total / (kSlots / hkv).  Where the tiles are fewer than the slots, they are split so that all
+// pieces run in one round; where they are more, only a tile of more than 1.5 shares is (a part
+// costs its rows' partial results, written and read).  Long pieces go first, in five classes of
+// length.  All waves compute the same from the same lengths.
+__device__ inline Piece find_piece(const Params& P, const int32_t* indptr, const int32_t* lens,
+                                   const int32_t* prefixes, int idx) {
+  const int lane = threadIdx.x & 63, per = (P.bs + 63) / 64;
+  int tiles[kPerLane], stages[kPerLane], splits[kPerLane], base[kPerLane], nth[kPerLane];
+  float cost = 0.f;
+  int count = 0;
+#pragma unroll
+  for (int i = 0; i < kPerLane; ++i) {
+    const int r = i * 64 + lane;
+    tiles[i] = stages[i] = 0;
+    splits[i] = 1;
+    if (i >= per || r >= P.bs) continue;
+    const int a = min(max(indptr[r], 0), P.total_q), b = min(max(indptr[r + 1], a), P.total_q);
+    const int L = min(max(lens[r], 0), P.max_len);
+    const int first = P.first && a < b ? min(max(P.first[a], 0), L) : 0;
+    const int seen = prefixes ? min(max(prefixes[r], 0), first) : 0;
+    tiles[i] = (int)(((int64_t)(b - a) * P.group + kRows - 1) / kRows);
+    stages[i] = max((L - first + seen + kStage - 1) / kStage, 1);
+    cost += (float)tiles[i] * stages[i];
+    count += tiles[i];
+  }
+  const auto add = [](float x, float y) { return x + y; };
+  const auto larger = [](float x, float y) { return fmaxf(x, y); };
+  const float total = last_lane(wave_scan(cost, 0.f, add));
+  const int items = last_lane(sum_scan(count));
+  if (P.max_places) {
+    const float slots = (float)kSlots / P.hkv;
+    const float limit = fmaxf(items < slots ? total / (slots - 0.5f * items) : 1.5f * total / slots, 4.f);
+    int places = 0, split_items = 0;
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) {
+      if (i >= per) continue;
+      splits[i] = min((int)ceilf(stages[i] / limit), kMaxSplits);
+      const int y = splits[i] > 1 ? tiles[i] : 0, x = y * splits[i];
+      const int upto = sum_scan(x), nth_upto = sum_scan(y);
+      base[i] = places + upto - x;
+      nth[i] = split_items + nth_upto - y;
+      places += last_lane(upto);
+      split_items += last_lane(nth_upto);
+    }
+    if (places > P.max_places) {   // cannot be, by the bound the host took
+#pragma unroll
+      for (int i = 0; i < kPerLane; ++i) splits[i] = 1;
+      split_items = 0;
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) *P.split_items = split_items;
+  }
+  int mine = 0;
+#pragma unroll
+  for (int i = 0; i < kPerLane; ++i) mine += tiles[i] * splits[i];
+  if (idx >= last_lane(sum_scan(mine))) return Piece{-1, 0, 0, 1, 0, 0};
+  float most = 0.f, each[kPerLane];
+#pragma unroll
+  for (int i = 0; i < kPerLane; ++i) {
+    each[i] = (float)stages[i] / splits[i];
+    if (tiles[i]) most = fmaxf(most, each[i]);
+  }
+  most = last_lane(wave_scan(most, 0.f, larger));
+  const float bounds[6] = {INFINITY, 0.75f * most, 0.5f * most, 0.35f * most, 0.2f * most, -1.f};
+  int before = 0;
+#pragma unroll
+  for (int k = 0; k < 5; ++k)
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) {
+      if (i >= per) continue;
+      const int x = each[i] <= bounds[k] && each[i] > bounds[k + 1] ? tiles[i] * splits[i] : 0;
+      const int upto = before + sum_scan(x);
+      const uint64_t m = __ballot(upto > idx);
+      if (m) {
+        const int l = __builtin_ctzll(m);
+        auto at = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+        const int local = idx - at(upto - x), n = at(splits[i]), t = at(tiles[i]);
+        Piece p;
+        p.r = i * 64 + l;
+        p.splits = n;
+        p.split = local % n;
+        p.tile = t - 1 - local / n;   // a request's last rows see the most tokens
+        p.place = n > 1 ? at(base[i]) + p.tile * n + p.split : 0;
+        p.record = n > 1 ? at(nth[i]) + p.tile : 0;
+        return p;
+      }
+      before = last_lane(upto);
+    }
+  return Piece{-1, 0, 0, 1, 0, 0};
 }
 
 // 1 KiB from src + OFFSET to dst + OFFSET, 16 bytes a lane.
@@ -442,15 +578,22 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   // heads fastest: with 8 KV heads the workgroups of a head share an XCD's L2
   const int x = blockIdx.x, g = x % P.hkv;
-  const int split = x / P.hkv % P.splits;
-  // a request's last items see the most tokens: they start first
-  const int item = P.items - 1 - x / P.hkv / P.splits;
-  const int r = find_request(P, indptr, item);
+  Piece piece;
+  if (P.parted) {
+    piece = find_piece(P, indptr, lens, prefixes, x / P.hkv);
+    if (piece.r < 0) return;
+  } else {
+    // the items as they come, the last first, none split
+    const int item = P.items - 1 - x / P.hkv;
+    const int r = find_request(P, indptr, item);
+    piece = Piece{r, item - first_item(P, indptr, r), 0, 1, 0, 0};
+  }
+  const int r = piece.r;
   const int a0 = min(max(indptr[r], 0), P.total_q);
   const int a1 = min(max(indptr[r + 1], a0), P.total_q);
   const int n = a1 - a0;
   const int64_t rows = (int64_t)n * P.group;
-  const int64_t row0 = (int64_t)(item - first_item(P, indptr, r)) * kRows;
+  const int64_t row0 = (int64_t)piece.tile * kRows;
   if (row0 < 0 || row0 >= rows) return;
   const int L = min(max(lens[r], 0),
                     min(P.max_len, P.width < (1 << 26) ? P.width * 16 : 1 << 30));
@@ -516,8 +659,8 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
   const int s2 = max(n1, from / kStage);
   const int n2 = to > 0 ? max((to + kStage - 1) / kStage - s2, 0) : 0;
   const int stages = n1 + n2;
-  const int per = (stages + P.splits - 1) / P.splits;
-  const int i0 = min(split * per, stages), i1 = min(i0 + per, stages);
+  const int per = (stages + piece.splits - 1) / piece.splits;
+  const int i0 = min(piece.split * per, stages), i1 = min(i0 + per, stages);
 
   Acc<D> a;
 #pragma unroll
@@ -719,12 +862,15 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
     a.l += other_half(a.l);
   }
 
+  const int64_t place = (int64_t)piece.place * P.hkv + g;
+  if (piece.splits > 1 && piece.split == 0 && tid == 0)
+    P.records[(int64_t)piece.record * P.hkv + g] =
+        make_int4(piece.splits | piece.place << 8, a0, (int)row0, count);
   if (!mine) return;
   const float l = a.l;
   const float f = l == 0.f ? 0.f : 1.f / l;   // no visible token: 0
-  const int64_t out_row = (int64_t)(a0 + j) * P.hq + g * P.group + h;
-  if (P.splits == 1) {
-    uint16_t* dst = P.out + out_row * D + (lane >> 5) * 4;
+  if (piece.splits == 1) {
+    uint16_t* dst = P.out + ((int64_t)(a0 + j) * P.hq + g * P.group + h) * D + (lane >> 5) * 4;
 #pragma unroll
     for (int t = 0; t < D / 32; ++t)
 #pragma unroll
@@ -736,7 +882,8 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
       }
     return;
   }
-  float* dst = P.part + ((int64_t)split * P.rows + out_row) * D + (lane >> 5) * 4;
+  const int64_t at = place * kRows + rg * kWaveRows + (lane & 31);
+  float* dst = P.part + at * D + (lane >> 5) * 4;
 #pragma unroll
   for (int t = 0; t < D / 32; ++t)
 #pragma unroll
@@ -744,24 +891,31 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
       float4 y = {a.o[t][4 * c] * f, a.o[t][4 * c + 1] * f, a.o[t][4 * c + 2] * f, a.o[t][4 * c + 3] * f};
       *(float4*)(dst + t * 32 + c * 8) = y;
     }
-  if (lane < 32) {
-    float2* ml = (float2*)(P.part + (int64_t)P.splits * P.rows * D) + (int64_t)split * P.rows + out_row;
-    *ml = make_float2(a.m, l);
-  }
+  if (lane < 32) P.part_ml[at] = make_float2(a.m, l);
 }
 
-// The splits of each row joined: D/4 threads take a row's columns, `teams` such teams (a power
-// of two) part its splits and meet in LDS.
+// The splits of an item's rows joined, 32 rows at a time: D/4 threads take a row's columns,
+// several such teams part many splits and meet in LDS.
 template <int D>
-__global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ part, uint16_t* out,
-                                                   int64_t rows, int splits, int teams) {
-  constexpr int kTeam = D / 4, kTeams = 256 / kTeam;
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(const Params P) {
+  constexpr int kTeam = D / 4, kTeams = kJoinThreads / kTeam;
   __shared__ float4 sums[kTeams][kTeam];
   __shared__ float2 meet[kTeams];   // (max, sum)
-  const int team = threadIdx.x / kTeam, c = threadIdx.x % kTeam, first = team & (teams - 1);
-  const int64_t row = (int64_t)blockIdx.x * (kTeams / teams) + team / teams;
-  const bool in = row < rows;
-  const float2* ml = (const float2*)(part + (int64_t)splits * rows * D);
+  const int team = threadIdx.x / kTeam, c = threadIdx.x % kTeam;
+  constexpr int kParts = kRows / 32;
+  const int units = *P.split_items * P.hkv * kParts;
+  for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
+  const int g = unit / kParts % P.hkv, part0 = unit % kParts * 32;
+  const int4 rec = P.records[unit / kParts];
+  const int splits = rec.x & 0xff, row1 = min(rec.w, part0 + 32);
+  if (part0 >= row1) continue;
+  const int64_t place = (int64_t)(rec.x >> 8) * P.hkv + g;
+  const int teams = splits > 16 ? 8 : splits > 8 ? 4 : splits > 4 ? 2 : 1;
+  const int first = team & (teams - 1);
+  for (int row0 = part0; row0 < row1; row0 += kTeams / teams) {
+  const int row = row0 + team / teams;
+  const bool in = row < row1;
+  const int64_t at = place * kRows + row, step = (int64_t)P.hkv * kRows;
   float m = -INFINITY, sum = 0.f;
   float4 o = {0.f, 0.f, 0.f, 0.f};
   for (int s0 = first; in && s0 < splits; s0 += 4 * teams) {
@@ -770,8 +924,8 @@ __global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ par
 #pragma unroll
     for (int u = 0; u < 4; ++u) {   // the four loads in flight; past the last split: nothing seen
       const int s = min(s0 + u * teams, splits - 1);
-      x[u] = ml[s * rows + row];
-      y[u] = *(const float4*)(part + (s * rows + row) * D + c * 4);
+      x[u] = P.part_ml[at + s * step];
+      y[u] = *(const float4*)(P.part + (at + s * step) * D + c * 4);
       if (s0 + u * teams >= splits || x[u].y == 0.f) x[u] = make_float2(-INFINITY, 0.f);
     }
     const float top = fmaxf(fmaxf(m, fmaxf(x[0].x, x[1].x)), fmaxf(x[2].x, x[3].x));
@@ -788,45 +942,57 @@ __global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ par
     }
   }
   if (teams > 1) {
+    __syncthreads();
     sums[team][c] = o;
     if (c == 0) meet[team] = make_float2(m, sum);
     __syncthreads();
-    if (first) return;
     float top = m;
-    for (int t = 1; t < teams; ++t) top = fmaxf(top, meet[team + t].x);
+    for (int t = 1; t < teams; ++t) top = fmaxf(top, meet[team - first + t].x);
     const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
     sum *= keep;
     o.x *= keep, o.y *= keep, o.z *= keep, o.w *= keep;
     for (int t = 1; t < teams; ++t) {
-      const float2 x = meet[team + t];
+      const float2 x = meet[team - first + t];
       if (x.x == -INFINITY) continue;
       const float f = __builtin_amdgcn_exp2f(x.x - top);
-      const float4 y = sums[team + t][c];
+      const float4 y = sums[team - first + t][c];
       sum += f * x.y;
       o.x += f * y.x, o.y += f * y.y, o.z += f * y.z, o.w += f * y.w;
     }
   }
-  if (!in) return;
-  const float f = sum == 0.f ? 0.f : 1.f / sum;
-  u32x2 y;
-  y[0] = pack(o.x * f, o.y * f);
-  y[1] = pack(o.z * f, o.w * f);
-  *(u32x2*)(out + row * D + c * 4) = y;
+  if (in && first == 0) {
+    const float f = sum == 0.f ? 0.f : 1.f / sum;
+    const int r = rec.z + row, j = r / P.group, h = r - j * P.group;
+    u32x2 y;
+    y[0] = pack(o.x * f, o.y * f);
+    y[1] = pack(o.z * f, o.w * f);
+    *(u32x2*)(P.out + ((int64_t)(rec.y + j) * P.hq + g * P.group + h) * D + c * 4) = y;
+  }
+  }
+  }
 }
 
-// Items of a batch (an upper bound) and the splits of their tokens.
+// Bounds per KV head: a batch's items, the split ones of them and their parts.
 struct Plan {
   int64_t items;
-  int splits;
+  int split_items, places;
 };
 
 Plan plan(int32_t bs, int32_t total_q, int32_t hq, int32_t hkv, int32_t max_len) {
   Plan p;
   p.items = (int64_t)total_q * (hq / hkv) / kRows + bs;
-  const int64_t groups = p.items * hkv, stages = ((int64_t)max_len + kStage - 1) / kStage;
-  // two workgroups a CU, at least four stages a split
-  int64_t s = std::min<int64_t>(512 / std::max<int64_t>(groups, 1), stages / 4);
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(s, 64));
+  // The second launch does not pay for itself where the items make two rounds or more, nor
+  // where they are short.
+  const int64_t stages = ((int64_t)max_len + kStage - 1) / kStage;
+  p.split_items = p.places = 0;
+  if (bs > kPartedBatch || p.items * hkv > 2 * kSlots || stages <= 12) return p;
+  // A tile of s stages has at most 1 + s / limit <= 2 s / limit parts if it is split, and the
+  // tiles' s sum to the total: at most 2 total / limit places, where limit is at least the
+  // share total / (kSlots / hkv); also at most kMaxSplits and ceil(stages / 4) a tile.
+  const int64_t share = 2 * kSlots / hkv + 1;
+  const int64_t each = std::min<int64_t>(kMaxSplits, (stages + 3) / 4);
+  p.places = (int)std::min(share, p.items * each);
+  p.split_items = (int)std::min<int64_t>(p.places / 2, p.items);
   return p;
 }
 
@@ -837,8 +1003,10 @@ bool sizes_ok(int32_t bs, int32_t total_q, int32_t hq, int32_t hkv, int32_t d, i
          (int64_t)total_q * hq <= INT32_MAX;
 }
 
-size_t workspace_bytes(const Plan& p, int32_t total_q, int32_t hq, int32_t d) {
-  return p.splits == 1 ? 0 : (size_t)p.splits * total_q * hq * (d + 2) * sizeof(float);
+size_t workspace_bytes(const Plan& p, int32_t hkv, int32_t d) {
+  // the count, the records, then (max, sum) and rows of every place
+  return p.places ? 16 + (size_t)p.split_items * hkv * 16 +
+                        (size_t)p.places * hkv * kRows * (8 + (size_t)d * 4) : 0;
 }
 
 }  // namespace
@@ -849,8 +1017,8 @@ extern "C" size_t nsd_chunk_attention_workspace_size(int32_t bs, int32_t total_q
                                                      int32_t max_seq_len) {
   if (!sizes_ok(bs, total_q, num_q_heads, num_kv_heads, head_dim, max_q_per_seq, max_seq_len))
     return 0;
-  return workspace_bytes(plan(bs, total_q, num_q_heads, num_kv_heads, max_seq_len), total_q,
-                         num_q_heads, head_dim);
+  return workspace_bytes(plan(bs, total_q, num_q_heads, num_kv_heads, max_seq_len), num_kv_heads,
+                         head_dim);
 }
 
 extern "C" nsd_status nsd_chunk_attention(
@@ -889,11 +1057,13 @@ extern "C" nsd_status nsd_chunk_attention(
   if (((uintptr_t)q | (uintptr_t)k_cache | (uintptr_t)v_cache | (uintptr_t)out) % 16)
     return fail(NSD_ERR_SHAPE, "%s: q, out and the caches must be 16-byte aligned", fn);
   const Plan pl = plan(bs, total_q, num_q_heads, num_kv_heads, max_seq_len);
-  const size_t need = workspace_bytes(pl, total_q, num_q_heads, head_dim);
+  const size_t need = workspace_bytes(pl, num_kv_heads, head_dim);
   if (need && (!workspace || workspace_size < need || (uintptr_t)workspace % 16))
     return fail(NSD_ERR_WORKSPACE, "%s: a 16-byte aligned workspace of %zu bytes needed, %zu given",
                 fn, need, workspace ? workspace_size : (size_t)0);
-  const int64_t groups = pl.items * num_kv_heads * pl.splits;
+  // parts beyond the first of each item: fewer than total / limit
+  const int64_t parts = std::min(pl.places, kSlots / num_kv_heads + 1);
+  const int64_t groups = (pl.items + parts) * num_kv_heads;
   if (groups > INT32_MAX) return fail(NSD_ERR_UNSUPPORTED, "%s: too many workgroups", fn);
   Params P;
   P.q = (const uint16_t*)q;
@@ -902,9 +1072,17 @@ extern "C" nsd_status nsd_chunk_attention(
   P.first = first_keys;
   P.slopes = slopes;
   P.out = (uint16_t*)out;
-  P.part = (float*)workspace;
+  const int64_t places = (int64_t)pl.places * num_kv_heads;
+  const int64_t split_items = (int64_t)pl.split_items * num_kv_heads;
+  P.split_items = (int32_t*)workspace;
+  P.records = (int4*)((char*)workspace + 16);
+  P.part_ml = (float2*)(P.records + split_items);
+  P.part = (float*)(P.part_ml + places * kRows);
+  P.max_places = pl.places;
+  // the order matters where the items do not all run at once and differ: among few requests,
+  // or more than find_piece() holds, they start as they come
+  P.parted = pl.places || (bs >= 16 && bs <= kPartedBatch && pl.items * num_kv_heads > kSlots);
   P.num_blocks = num_blocks;
-  P.rows = (int64_t)total_q * num_q_heads;
   // 0 becomes a factor too small to move a weight, as 0 times a hidden token's -infinity is NaN
   P.scale = std::max(std::fabs(scale) * kLog2e, 1e-37f);
   P.cap = softcap;
@@ -917,7 +1095,6 @@ extern "C" nsd_status nsd_chunk_attention(
   P.group = num_q_heads / num_kv_heads;
   P.max_len = num_blocks ? max_seq_len : 0;   // without a pool nothing is visible
   P.items = (int32_t)pl.items;
-  P.splits = pl.splits;
   clear_stale_error();
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((uint32_t)groups), dim3(kThreads), 0, (hipStream_t)stream, P,
@@ -932,17 +1109,13 @@ extern "C" nsd_status nsd_chunk_attention(
     else bias ? go(chunk_kernel<128, false, true>) : go(chunk_kernel<128, false, false>);
   }
   if (const nsd_status st = check_launch(fn)) return st;
-  if (pl.splits > 1) {
-    const int most = 1024 / head_dim;
-    int teams = 1;
-    while (teams < most && teams * 4 < pl.splits) teams *= 2;
-    const int per = most / teams;
-    const dim3 grid((uint32_t)((P.rows + per - 1) / per));
-    auto join = [&](auto kernel) {
-      hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, P.part, P.out, P.rows,
-                         pl.splits, teams);
-    };
-    head_dim == 64 ? join(join_kernel<64>) : join(join_kernel<128>);
+  if (pl.places) {
+    // at most a workgroup a CU, each taking several items' rows in turn
+    const dim3 grid((uint32_t)std::min<int64_t>(split_items * (kRows / 32), kSlots / 2));
+    if (head_dim == 64)
+      hipLaunchKernelGGL(join_kernel<64>, grid, dim3(kJoinThreads), 0, (hipStream_t)stream, P);
+    else
+      hipLaunchKernelGGL(join_kernel<128>, grid, dim3(kJoinThreads), 0, (hipStream_t)stream, P);
     return check_launch(fn);
   }
   return NSD_OK;
