@@ -9,16 +9,20 @@
 // fractional turn left in fp32 (its steps are 0.06 there), so the angle is
 // formed and reduced to a turn in fp64, once per row and pair for all heads.
 //
-// The work is memory traffic: (2 Hq + 4 Hkv) D 2 bytes a row.  A workgroup
-// takes `rows_per` consecutive rows and `heads_per` KV heads with their query
-// heads: all heads share its angles in LDS.  The cache's K plane takes a row's
-// 8 dimensions as 16 bytes with the slots adjacent, its V plane 2 bytes a row
-// with the 16 slots of a dimension adjacent, so rows that follow each other in
-// one block (a run) are written together, a whole 32-byte V sector where the
-// run fills its block.  A run is at most 16 rows; the workgroup whose rows
-// hold its first row takes all of it.  Slots that a run does not fill are not
-// touched (narrower stores), so rows may name slots in any order.
+// The work is memory traffic: (2 Hq + 4 Hkv) D 2 bytes a row.  Workgroups are of three kinds, so
+// that each waits for as few loads in a row as it can: query rows (angles, no slots), key rows
+// (both) and value rows (slots, no angles).  One takes `rows` consecutive rows and some heads,
+// which share the angles in LDS.
+//
+// The cache's K plane takes a row's 8 dimensions as 16 bytes with the slots adjacent, its V plane
+// 2 bytes a row with the 16 slots of a dimension adjacent, so value rows that follow each other
+// in one block (a run) are written together, a whole 32-byte V sector where the run fills its
+// block.  A run is at most 16 rows; the workgroup whose rows hold its first row takes all of
+// it.  Slots that a run does not fill are not touched (narrower stores), so rows may name slots
+// in any order.
 #include "nsd_internal.h"
+
+#include <algorithm>
 
 namespace {
 
@@ -32,6 +36,11 @@ constexpr int kMaxAxes = 4;
 constexpr int kRows = 16;              // rows of a workgroup, at most
 constexpr int kSpan = kRows + 15;      // with the rest of a run begun in them
 
+// The grid's part of one kind: `heads` heads a workgroup, `groups` such groups.
+struct Kind {
+  int32_t first, heads, groups;
+};
+
 struct RopeArgs {
   const uint16_t *q, *k, *v;
   uint16_t *q_out, *k_pool, *v_pool;
@@ -40,7 +49,8 @@ struct RopeArgs {
   int64_t q_stride, k_stride, v_stride;   // elements between rows
   int64_t num_slots;
   int32_t cuts[kMaxAxes];                 // pairs below cuts[a] belong to axes up to a
-  int32_t total, hq, hkv, rot, rows_per, heads_per;
+  int32_t total, hq, hkv, rot, rows;      // rows of a workgroup: a power of two
+  Kind query, key, value;
 };
 
 __device__ inline float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
@@ -89,39 +99,13 @@ __device__ inline bool unit(int c, int rot, int* x, int* y) {
   return turned;
 }
 
-template <int D, bool ADJ>
-__global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeArgs A) {
-  __shared__ float2 turns[kSpan][D / 2];   // (cos, sin)
-  __shared__ int32_t slot[kSpan], first[kSpan + 1];   // rows' slots; runs' first rows
-  __shared__ int32_t span[2], runs;
-  const int tid = threadIdx.x;
-  const int64_t i0 = (int64_t)blockIdx.x * A.rows_per;
-  const int g0 = blockIdx.y * A.heads_per, gn = min(A.heads_per, A.hkv - g0);
-  // rows [begin, end): from the first run begun at or after i0 to the first begun at or
-  // after i0 + rows_per
-  if (tid < 64) {
-    const int64_t i = i0 + tid;
-    const bool b = tid < kSpan + 1 && (i >= A.total || begins(A.slots, i));
-    const uint64_t m = __ballot(b);
-    // a run is at most 16 rows, so both searches end within 16
-    const int lo = __builtin_ctzll(m), hi = A.rows_per + __builtin_ctzll(m >> A.rows_per);
-    if (tid == 0) {
-      span[0] = lo;
-      span[1] = min(hi, (int)min(A.total - i0, (int64_t)kSpan));
-    }
-    const bool mine = b && tid >= lo && tid < hi && i < A.total;
-    const uint64_t mm = __ballot(mine);
-    if (mine) first[__popcll(mm & ((1ull << tid) - 1))] = tid;
-    if (tid == 0) runs = __popcll(mm);
-    if (tid < kSpan) slot[tid] = i < A.total ? A.slots[i] : -1;
-  }
-  __syncthreads();
-  const int lo = span[0], n = span[1] - lo;   // rows i0 + lo + [0, n)
-  if (n <= 0) return;
-  const int64_t base = i0 + lo;
+// (cos, sin) of rows base .. base + n - 1.
+template <int D>
+__device__ inline void angles(const RopeArgs& A, int64_t base, int n, float2 (*turns)[D / 2]) {
   const int pairs = A.rot / 2;
-  for (int u = tid; u < n * pairs; u += kThreads) {
-    const int row = u / pairs, p = u - row * pairs;
+  for (int u = threadIdx.x; u < n * (D / 2); u += kThreads) {
+    const int row = u / (D / 2), p = u % (D / 2);
+    if (p >= pairs) continue;
     int axis = 0;
 #pragma unroll
     for (int a = 0; a < kMaxAxes - 1; ++a) axis += p >= A.cuts[a];
@@ -131,58 +115,122 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeArgs A) {
     sincospif((float)(2.0 * (t - rint(t))), &s, &c);
     turns[row][p] = make_float2(c, s);
   }
+}
+
+// 16 dimensions of a row: loaded, turned where they are, and their places in the head.
+template <int D, bool ADJ>
+struct Unit {
+  u32x4 x, y;
+  int xo, yo;
+  bool turned;
+  __device__ inline void load(const uint16_t* head, int c, int rot) {
+    turned = unit<ADJ>(c, rot, &xo, &yo);
+    x = *(const u32x4*)(head + xo);
+    y = *(const u32x4*)(head + yo);
+  }
+  __device__ inline void turn(const float2* cs) {
+    if (!turned) return;
+    if (ADJ) turn_adjacent(x, y, cs);
+    else turn_half(x, y, cs);
+  }
+};
+
+template <int D, bool ADJ>
+__device__ inline void query_rows(const RopeArgs& A, int64_t base, int g, float2 (*turns)[D / 2]) {
+  constexpr int U = D / 16, kStep = kThreads / U;
+  const int n = (int)min((int64_t)A.rows, A.total - base);
+  const int h0 = g * A.query.heads, hn = min(A.query.heads, A.hq - h0);
+  const int c = threadIdx.x % U, units = n * hn;
+  // this thread's (row, head)s, kStep units apart; the first one's row is loaded under the angles
+  int i = threadIdx.x / U, row = i / hn, h = i - row * hn;
+  const int row_step = kStep / hn, h_step = kStep - row_step * hn;
+  Unit<D, ADJ> x;
+  auto load = [&] { x.load(A.q + (base + row) * A.q_stride + (h0 + h) * D, c, A.rot); };
+  if (i < units) load();
+  angles<D>(A, base, n, turns);
   __syncthreads();
-  const int group = A.hq / A.hkv;
+  while (i < units) {
+    x.turn(&turns[row][8 * c]);
+    uint16_t* dst = A.q_out + ((base + row) * A.hq + h0 + h) * D;
+    *(u32x4*)(dst + x.xo) = x.x;
+    *(u32x4*)(dst + x.yo) = x.y;
+    i += kStep;
+    row += row_step;
+    h += h_step;
+    if (h >= hn) h -= hn, ++row;
+    if (i < units) load();
+  }
+}
+
+template <int D, bool ADJ>
+__device__ inline void key_rows(const RopeArgs& A, int64_t base, int g, float2 (*turns)[D / 2]) {
   constexpr int U = D / 16;
-  // query rows
-  const int qh = gn * group;
-  for (int u = tid; u < n * qh * U; u += kThreads) {
-    const int c = u % U, h = u / U % qh, row = u / U / qh;
-    int xo, yo;
-    const bool turned = unit<ADJ>(c, A.rot, &xo, &yo);
-    const int64_t head = (int64_t)(g0 * group + h) * D;
-    const uint16_t* src = A.q + (base + row) * A.q_stride + head;
-    u32x4 x = *(const u32x4*)(src + xo), y = *(const u32x4*)(src + yo);
-    if (turned) {
-      if (ADJ) turn_adjacent(x, y, &turns[row][8 * c]);
-      else turn_half(x, y, &turns[row][8 * c]);
+  const int n = (int)min((int64_t)A.rows, A.total - base);
+  const int g0 = g * A.key.heads, gn = min(A.key.heads, A.hkv - g0);
+  // neighbouring lanes take neighbouring rows, whose slots are adjacent in the plane
+  const int row = threadIdx.x & (A.rows - 1), step = kThreads / A.rows;
+  int i = threadIdx.x / A.rows;
+  const int units = row < n ? gn * U : 0;
+  const int64_t s = row < n ? A.slots[base + row] : -1;
+  Unit<D, ADJ> x;
+  auto load = [&] {
+    x.load(A.k + (base + row) * A.k_stride + (g0 + i / U) * D, i % U, A.rot);
+  };
+  if (i < units) load();
+  angles<D>(A, base, n, turns);
+  __syncthreads();
+  const bool cached = s >= 0 && s < A.num_slots;
+  while (i < units) {
+    x.turn(&turns[row][8 * (i % U)]);
+    if (cached) {
+      uint16_t* dst = A.k_pool + (s / 16 * A.hkv + g0 + i / U) * (D * 16) + s % 16 * 8;
+      *(u32x4*)(dst + x.xo * 16) = x.x;
+      *(u32x4*)(dst + x.yo * 16) = x.y;
     }
-    uint16_t* dst = A.q_out + (base + row) * A.hq * D + head;
-    *(u32x4*)(dst + xo) = x;
-    *(u32x4*)(dst + yo) = y;
+    i += step;
+    if (i < units) load();
   }
-  // key rows: neighbouring lanes take neighbouring rows, whose slots are adjacent in the plane
-  for (int u = tid; u < n * gn * U; u += kThreads) {
-    const int row = u % n, c = u / n % U, g = g0 + u / n / U;
-    const int64_t s = slot[lo + row];
-    if (s < 0 || s >= A.num_slots) continue;
-    int xo, yo;
-    const bool turned = unit<ADJ>(c, A.rot, &xo, &yo);
-    const uint16_t* src = A.k + (base + row) * A.k_stride + (int64_t)g * D;
-    u32x4 x = *(const u32x4*)(src + xo), y = *(const u32x4*)(src + yo);
-    if (turned) {
-      if (ADJ) turn_adjacent(x, y, &turns[row][8 * c]);
-      else turn_half(x, y, &turns[row][8 * c]);
+}
+
+template <int D>
+__device__ inline void value_rows(const RopeArgs& A, int64_t i0, int g) {
+  __shared__ int32_t slot[kSpan], first[kSpan + 1];   // rows' slots; runs' first rows
+  __shared__ int32_t span[2];                         // past the last row; runs
+  const int tid = threadIdx.x;
+  const int g0 = g * A.value.heads, gn = min(A.value.heads, A.hkv - g0);
+  // rows from the first run begun at or after i0 to the first begun at or after i0 + rows
+  if (tid < 64) {
+    const int64_t i = i0 + tid;
+    const bool b = tid < kSpan + 1 && (i >= A.total || begins(A.slots, i));
+    const uint64_t m = __ballot(b);
+    // a run is at most 16 rows, so both searches end within 16
+    const int lo = __builtin_ctzll(m), hi = A.rows + __builtin_ctzll(m >> A.rows);
+    const bool mine = b && tid >= lo && tid < hi && i < A.total;
+    const uint64_t mm = __ballot(mine);
+    if (mine) first[__popcll(mm & ((1ull << tid) - 1))] = tid;
+    if (tid < kSpan) slot[tid] = i < A.total ? A.slots[i] : -1;
+    if (tid == 0) {
+      span[0] = min(hi, (int)min(A.total - i0, (int64_t)kSpan));
+      span[1] = __popcll(mm);
     }
-    uint16_t* dst = A.k_pool + (s / 16 * A.hkv + g) * (D * 16) + s % 16 * 8;
-    *(u32x4*)(dst + xo * 16) = x;
-    *(u32x4*)(dst + yo * 16) = y;
   }
-  // value rows: two dimensions of a run
+  __syncthreads();
+  const int runs = span[1];
+  // two dimensions of a run
   for (int u = tid; u < runs * gn * (D / 2); u += kThreads) {
-    const int c = u % (D / 2), g = g0 + u / (D / 2) % gn, run = u / (D / 2) / gn;
-    const int a = first[run], b = run + 1 < runs ? first[run + 1] : span[1];
+    const int c = u % (D / 2), v = u / (D / 2), run = v / gn, head = g0 + v - run * gn;
+    const int a = first[run], b = run + 1 < runs ? first[run + 1] : span[0];
     const int64_t s = slot[a];
     if (s < 0 || s >= A.num_slots) continue;
     const int s0 = (int)(s % 16);
-    const uint16_t* src = A.v + (base + (a - lo)) * A.v_stride + (int64_t)g * D + 2 * c;
+    const uint16_t* src = A.v + (i0 + a) * A.v_stride + head * D + 2 * c;
+    uint16_t* dst = A.v_pool + ((s / 16 * A.hkv + head) * D + 2 * c) * 16;
     uint32_t w[16];
 #pragma unroll
     for (int p = 0; p < 16; ++p) {
       const int j = p - s0;
       w[p] = j >= 0 && j < b - a ? *(const uint32_t*)(src + j * A.v_stride) : 0u;
     }
-    uint16_t* dst = A.v_pool + ((s / 16 * A.hkv + g) * D + 2 * c) * 16;
     if (s0 == 0 && b - a == 16) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -204,6 +252,28 @@ __global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeArgs A) {
         dst[16 + p] = (uint16_t)(w[p] >> 16);
       }
     }
+  }
+}
+
+template <int D, bool ADJ>
+__global__ __launch_bounds__(kThreads) void rope_append_kernel(RopeArgs A) {
+  __shared__ float2 turns[kRows][D / 2];
+  const int b = blockIdx.x;
+  auto place = [&](const Kind& k, int* g) {
+    const int i = b - k.first;
+    *g = i % k.groups;
+    return (int64_t)(i / k.groups) * A.rows;
+  };
+  int g;
+  if (b < A.key.first) {
+    const int64_t base = place(A.query, &g);
+    query_rows<D, ADJ>(A, base, g, turns);
+  } else if (b < A.value.first) {
+    const int64_t base = place(A.key, &g);
+    key_rows<D, ADJ>(A, base, g, turns);
+  } else {
+    const int64_t base = place(A.value, &g);
+    value_rows<D>(A, base, g);
   }
 }
 
@@ -282,10 +352,25 @@ extern "C" nsd_status nsd_rope_append(void* k_pool, void* v_pool, int64_t num_bl
   A.hq = num_q_heads;
   A.hkv = num_kv_heads;
   A.rot = rot_dim;
-  A.rows_per = kRows;
-  A.heads_per = 1;
-  const dim3 grid((uint32_t)(((int64_t)total_q + A.rows_per - 1) / A.rows_per),
-                  (uint32_t)((num_kv_heads + A.heads_per - 1) / A.heads_per));
+  // Few rows: few of them a workgroup, and a workgroup for each group of heads, until the device
+  // has enough workgroups.
+  A.rows = total_q <= 256 ? 4 : kRows;
+  const int64_t tiles = ((int64_t)total_q + A.rows - 1) / A.rows;
+  int64_t blocks = 0;
+  auto kind = [&](int32_t heads, int32_t most) {
+    Kind k;
+    k.first = (int32_t)blocks;
+    k.heads = std::min(heads, most);
+    while (k.heads > 1 && tiles * ((heads + k.heads - 1) / k.heads) < 1024) k.heads = (k.heads + 1) / 2;
+    k.groups = (heads + k.heads - 1) / k.heads;
+    blocks += tiles * k.groups;
+    return k;
+  };
+  A.query = kind(num_q_heads, 32);
+  A.key = kind(num_kv_heads, 32);
+  A.value = kind(num_kv_heads, 32);
+  if (blocks > INT32_MAX) return fail(NSD_ERR_UNSUPPORTED, "%s: too many workgroups", fn);
+  const dim3 grid((uint32_t)blocks);
   clear_stale_error();
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, (hipStream_t)stream, A);
