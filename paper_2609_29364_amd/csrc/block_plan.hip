@@ -21,11 +21,12 @@
 // scan, and several leave aliased ones to a second launch.
 #include "nsd_internal.h"
 
+#include <type_traits>
+
 namespace {
 
 constexpr int kThreads = 1024;
 constexpr int kMaxBatch = 8192;
-constexpr int kPer = kMaxBatch / kThreads;   // requests per thread, at most
 
 // Inclusive prefix sum over the workgroup's threads.
 __device__ inline int64_t scan(int64_t x, int64_t* part) {
@@ -61,56 +62,69 @@ struct PlanArgs {
   int32_t width, capacity, bs, total_q;
 };
 
-// LDS: indptr, start, lens, owned, each of bs + 1 entries.
+// PER: requests per thread.  LDS: indptr, start, lens, owned, each of bs + 1 entries.
+template <int PER>
 __global__ __launch_bounds__(kThreads) void plan_kernel(PlanArgs A, int counters, int rows) {
   extern __shared__ int32_t mem[];
   __shared__ int64_t part[kThreads / 64];
-  __shared__ int32_t used;
+  __shared__ int32_t taken[kThreads / 64];   // by each wave's last granted request
   const int n = A.bs, tid = threadIdx.x;
   int32_t *indptr = mem, *start = mem + (n + 1), *lens = mem + 2 * (n + 1),
           *owned = mem + 3 * (n + 1);
-  const int per = (n + kThreads - 1) / kThreads;
   const int free_n = min(max(A.free_count[0], 0), A.capacity);
-  if (tid == 0) used = 0;
-  int64_t need[kPer], sum = 0;
-  bool wide[kPer];   // more tokens than the table's row holds
+  int a[PER], count[PER], len[PER], own[PER];
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int r = tid * per + i;
-    need[i] = 0;
-    wide[i] = false;
-    if (i >= per || r >= n) continue;
-    const int a = min(max(A.indptr[r], 0), A.total_q);
-    const int b = min(max(A.indptr[r + 1], a), A.total_q);
-    const int l = max(A.lens[r], 0), o = min(max(A.owned[r], 0), A.width);
-    const int64_t blocks = ((int64_t)l + (b - a) + NSD_BLOCK_SIZE - 1) / NSD_BLOCK_SIZE;
-    indptr[r] = a;
-    lens[r] = l;
-    owned[r] = o;
+  for (int i = 0; i < PER; ++i) {   // (all the loads in flight)
+    const int r = min(tid * PER + i, n - 1);
+    a[i] = n ? A.indptr[r] : 0;
+    count[i] = n ? A.indptr[r + 1] : 0;
+    len[i] = n ? A.lens[r] : 0;
+    own[i] = n ? A.owned[r] : 0;
+  }
+  int64_t need[PER], sum = 0;
+  bool wide[PER];   // more tokens than the table's row holds
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int r = tid * PER + i;
+    a[i] = min(max(a[i], 0), A.total_q);
+    count[i] = min(max(count[i], a[i]), A.total_q) - a[i];
+    len[i] = max(len[i], 0);
+    own[i] = min(max(own[i], 0), A.width);
+    const int64_t blocks = ((int64_t)len[i] + count[i] + NSD_BLOCK_SIZE - 1) / NSD_BLOCK_SIZE;
     wide[i] = blocks > A.width;
-    need[i] = wide[i] ? 0 : max(blocks - o, (int64_t)0);
+    need[i] = wide[i] || r >= n ? 0 : max(blocks - own[i], (int64_t)0);
     sum += need[i];
+    if (r < n) {
+      indptr[r] = a[i];
+      lens[r] = len[i];
+    }
   }
   int64_t upto = scan(sum, part) - sum;
+  int32_t mine = 0;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int r = tid * per + i;
-    if (i >= per || r >= n) continue;
+  for (int i = 0; i < PER; ++i) {
+    const int r = tid * PER + i;
     const int64_t before = upto;
     upto += need[i];
     const bool ok = !wide[i] && (need[i] == 0 || upto <= free_n);
+    if (r >= n) continue;
     // past the granted requests the prefix stays above every granted block's number
     start[r] = (int32_t)min(before, (int64_t)free_n);
-    if (ok && need[i]) atomicMax(&used, (int32_t)upto);
+    owned[r] = ok ? own[i] : -1;
+    if (ok && need[i]) mine = (int32_t)upto;
     if (counters && blockIdx.x == 0) {
-      const int count = min(max(A.indptr[r + 1], indptr[r]), A.total_q) - indptr[r];
       A.granted[r] = ok;
-      A.new_owned[r] = owned[r] + (ok ? (int32_t)need[i] : 0);
-      A.new_lens[r] = lens[r] + (ok ? count : 0);
+      A.new_owned[r] = own[i] + (ok ? (int32_t)need[i] : 0);
+      A.new_lens[r] = len[i] + (ok ? count[i] : 0);
     }
-    if (!ok) owned[r] = -1;
   }
+  // the ids taken: up to the last granted request that needs some (the prefix does not fall)
+  const uint64_t m = __ballot(mine > 0);
+  if ((tid & 63) == (m ? 63 - __builtin_clzll(m) : 0)) taken[tid >> 6] = mine;
   __syncthreads();
+  int32_t used = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) used = max(used, taken[w]);
   if (counters && blockIdx.x == 0 && tid == 0) A.new_count[0] = free_n - used;
   if (!rows) return;
   const int at = blockIdx.x * kThreads + tid, step = gridDim.x * kThreads;
@@ -144,37 +158,40 @@ struct TrimArgs {
 };
 
 // LDS: start, kept, each of bs + 1 entries.
+template <int PER>
 __global__ __launch_bounds__(kThreads) void trim_kernel(TrimArgs A, int counters, int rows) {
   extern __shared__ int32_t mem[];
   __shared__ int64_t part[kThreads / 64];
   __shared__ int32_t total;
   const int n = A.bs, tid = threadIdx.x;
   int32_t *start = mem, *kept = mem + (n + 1);
-  const int per = (n + kThreads - 1) / kThreads;
   const int free_n = min(max(A.free_count[0], 0), A.capacity);
-  int32_t back[kPer];
+  int32_t own[PER], keep[PER], back[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {   // (all the loads in flight)
+    const int r = min(tid * PER + i, n - 1);
+    own[i] = n ? A.owned[r] : 0;
+    keep[i] = n ? A.keep[r] : 0;
+  }
   int64_t sum = 0;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int r = tid * per + i;
-    back[i] = 0;
-    if (i >= per || r >= n) continue;
-    const int o = min(max(A.owned[r], 0), A.width);
-    const int64_t b = ((int64_t)max(A.keep[r], 0) + NSD_BLOCK_SIZE - 1) / NSD_BLOCK_SIZE;
-    const int k = (int)min((int64_t)o, b);
-    kept[r] = k;
-    back[i] = o - k;
+  for (int i = 0; i < PER; ++i) {
+    const int o = min(max(own[i], 0), A.width);
+    const int64_t b = ((int64_t)max(keep[i], 0) + NSD_BLOCK_SIZE - 1) / NSD_BLOCK_SIZE;
+    keep[i] = (int)min((int64_t)o, b);
+    back[i] = tid * PER + i < n ? o - keep[i] : 0;
     sum += back[i];
   }
   const int64_t end = scan(sum, part);
   int64_t upto = end - sum;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int r = tid * per + i;
-    if (i >= per || r >= n) continue;
+  for (int i = 0; i < PER; ++i) {
+    const int r = tid * PER + i;
+    if (r >= n) continue;
     start[r] = (int32_t)upto;
+    kept[r] = keep[i];
     upto += back[i];
-    if (counters && blockIdx.x == 0) A.new_owned[r] = kept[r];
+    if (counters && blockIdx.x == 0) A.new_owned[r] = keep[i];
   }
   // ids past the list's capacity are dropped
   if (tid == kThreads - 1) total = (int32_t)min(end, (int64_t)(A.capacity - free_n));
@@ -193,17 +210,24 @@ int groups(int64_t work) {
   return (int)(g < 256 ? g : 256);
 }
 
-// Runs kernel(args, counters, rows) over the work, the counters in the same launch unless
-// several workgroups would still read what they overwrite.
+// Runs kernel(requests per thread)(args, counters, rows) over the work, the counters in the
+// same launch unless several workgroups would still read what they overwrite.
 template <class Kernel, class Args>
 void launch(Kernel kernel, const Args& args, int64_t work, bool alias, size_t lds,
             hipStream_t stream) {
   const int g = groups(work);
   const bool apart = g > 1 && alias;
-  hipLaunchKernelGGL(kernel, dim3(g), dim3(kThreads), lds, stream, args, apart ? 0 : 1, 1);
-  if (apart)
-    hipLaunchKernelGGL(kernel, dim3(1), dim3(kThreads), lds, stream, args, 1, 0);
+  auto go = [&](auto k) {
+    hipLaunchKernelGGL(k, dim3(g), dim3(kThreads), lds, stream, args, apart ? 0 : 1, 1);
+    if (apart) hipLaunchKernelGGL(k, dim3(1), dim3(kThreads), lds, stream, args, 1, 0);
+  };
+  using std::integral_constant;
+  if (args.bs <= kThreads) go(kernel(integral_constant<int, 1>{}));
+  else if (args.bs <= 2 * kThreads) go(kernel(integral_constant<int, 2>{}));
+  else if (args.bs <= 4 * kThreads) go(kernel(integral_constant<int, 4>{}));
+  else go(kernel(integral_constant<int, 8>{}));
 }
+static_assert(kMaxBatch == 8 * kThreads, "a thread takes at most 8 requests");
 
 nsd_status check_sizes(const char* fn, int32_t bs, int32_t width, int32_t capacity) {
   using namespace nsd;
@@ -238,7 +262,7 @@ extern "C" nsd_status nsd_plan_blocks(int32_t* block_table, int32_t max_blocks_p
                       free_capacity, bs, bs ? total_q : 0};
   const bool alias = new_owned == owned || new_lens == seq_lens || new_free_count == free_count;
   clear_stale_error();
-  launch(plan_kernel, args, args.total_q, alias, ((size_t)bs + 1) * 16, (hipStream_t)stream);
+  launch([](auto per) { return plan_kernel<decltype(per)::value>; }, args, args.total_q, alias, ((size_t)bs + 1) * 16, (hipStream_t)stream);
   return check_launch(fn);
 }
 
@@ -261,7 +285,7 @@ extern "C" nsd_status nsd_trim_blocks(const int32_t* block_table, int32_t max_bl
   clear_stale_error();
   // the host does not know how many blocks come back: at most the tables' or the list's
   const int64_t most = (int64_t)bs * max_blocks_per_seq;
-  launch(trim_kernel, args, most < free_capacity ? most : free_capacity, alias,
+  launch([](auto per) { return trim_kernel<decltype(per)::value>; }, args, most < free_capacity ? most : free_capacity, alias,
          ((size_t)bs + 1) * 8, (hipStream_t)stream);
   return check_launch(fn);
 }

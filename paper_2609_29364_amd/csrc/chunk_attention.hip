@@ -156,18 +156,30 @@ __device__ inline Piece find_piece(const Params& P, const int32_t* indptr, const
   int tiles[kPerLane], stages[kPerLane], splits[kPerLane], base[kPerLane], nth[kPerLane];
   float cost = 0.f;
   int count = 0;
+  int a[kPerLane], b[kPerLane], L[kPerLane], prefix[kPerLane], first[kPerLane];
+#pragma unroll
+  for (int i = 0; i < kPerLane; ++i) {   // (all the loads in flight)
+    const int r = min(i * 64 + lane, P.bs - 1);
+    a[i] = indptr[r];
+    b[i] = indptr[r + 1];
+    L[i] = lens[r];
+    prefix[i] = prefixes ? prefixes[r] : 0;
+  }
 #pragma unroll
   for (int i = 0; i < kPerLane; ++i) {
-    const int r = i * 64 + lane;
-    tiles[i] = stages[i] = 0;
+    a[i] = min(max(a[i], 0), P.total_q);
+    b[i] = min(max(b[i], a[i]), P.total_q);
+    first[i] = P.first ? P.first[min(a[i], P.total_q - 1)] : 0;
+  }
+#pragma unroll
+  for (int i = 0; i < kPerLane; ++i) {
+    const bool in = i * 64 + lane < P.bs;
+    const int length = min(max(L[i], 0), P.max_len);
+    const int from = min(max(first[i], 0), length);
+    const int seen = min(max(prefix[i], 0), from);
+    tiles[i] = in ? (int)(((int64_t)(b[i] - a[i]) * P.group + kRows - 1) / kRows) : 0;
+    stages[i] = in ? max((length - from + seen + kStage - 1) / kStage, 1) : 0;
     splits[i] = 1;
-    if (i >= per || r >= P.bs) continue;
-    const int a = min(max(indptr[r], 0), P.total_q), b = min(max(indptr[r + 1], a), P.total_q);
-    const int L = min(max(lens[r], 0), P.max_len);
-    const int first = P.first && a < b ? min(max(P.first[a], 0), L) : 0;
-    const int seen = prefixes ? min(max(prefixes[r], 0), first) : 0;
-    tiles[i] = (int)(((int64_t)(b - a) * P.group + kRows - 1) / kRows);
-    stages[i] = max((L - first + seen + kStage - 1) / kStage, 1);
     cost += (float)tiles[i] * stages[i];
     count += tiles[i];
   }

@@ -192,6 +192,34 @@ __device__ inline void key_rows(const RopeArgs& A, int64_t base, int g, float2 (
   }
 }
 
+// Slots [s0, s1) of a dimension's 16 (w: all 16, in pairs), in the widest stores that hold no
+// other slot: a store of 2 bytes costs as much as one of 16.
+__device__ inline void put_run(uint16_t* dst, const u32x4 (&w)[2], int s0, int s1) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (s0 <= 8 * h && s1 >= 8 * h + 8) {
+      *(u32x4*)(dst + 8 * h) = w[h];
+      continue;
+    }
+#pragma unroll
+    for (int f = 0; f < 2; ++f) {
+      const int t = 8 * h + 4 * f;
+      if (s0 <= t && s1 >= t + 4) {
+        *(u32x2*)(dst + t) = u32x2{w[h][2 * f], w[h][2 * f + 1]};
+        continue;
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int p = t + 2 * e;
+        const uint32_t x = w[h][2 * f + e];
+        if (s0 <= p && s1 >= p + 2) *(uint32_t*)(dst + p) = x;
+        else if (s0 <= p && s1 == p + 1) dst[p] = (uint16_t)x;
+        else if (s0 == p + 1 && s1 >= p + 2) dst[p + 1] = (uint16_t)(x >> 16);
+      }
+    }
+  }
+}
+
 template <int D>
 __device__ inline void value_rows(const RopeArgs& A, int64_t i0, int g) {
   __shared__ int32_t slot[kSpan], first[kSpan + 1];   // rows' slots; runs' first rows
@@ -225,33 +253,26 @@ __device__ inline void value_rows(const RopeArgs& A, int64_t i0, int g) {
     const int s0 = (int)(s % 16);
     const uint16_t* src = A.v + (i0 + a) * A.v_stride + head * D + 2 * c;
     uint16_t* dst = A.v_pool + ((s / 16 * A.hkv + head) * D + 2 * c) * 16;
-    uint32_t w[16];
-#pragma unroll
-    for (int p = 0; p < 16; ++p) {
-      const int j = p - s0;
-      w[p] = j >= 0 && j < b - a ? *(const uint32_t*)(src + j * A.v_stride) : 0u;
+    if (b - a == 1) {   // a single token
+      const uint32_t x = *(const uint32_t*)src;
+      dst[s0] = (uint16_t)x;
+      dst[16 + s0] = (uint16_t)(x >> 16);
+      continue;
     }
-    if (s0 == 0 && b - a == 16) {
+    uint32_t w[16];   // slots beside the run get some row of it: no load waits for a comparison
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        u32x4 even, odd;
+    for (int p = 0; p < 16; ++p)
+      w[p] = *(const uint32_t*)(src + min(max(p - s0, 0), b - a - 1) * A.v_stride);
+    // the two dimensions' slots, in pairs; [s0, s1) are the run's
+    u32x4 even[2], odd[2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t p = w[8 * h + 2 * e], q = w[8 * h + 2 * e + 1];
-          even[e] = (p & 0xffffu) | q << 16;
-          odd[e] = p >> 16 | (q & 0xffff0000u);
-        }
-        ((u32x4*)dst)[h] = even;
-        ((u32x4*)dst)[2 + h] = odd;
-      }
-    } else {
-#pragma unroll
-      for (int p = 0; p < 16; ++p) {
-        if (p < s0 || p >= s0 + (b - a)) continue;
-        dst[p] = (uint16_t)w[p];
-        dst[16 + p] = (uint16_t)(w[p] >> 16);
-      }
+    for (int e = 0; e < 8; ++e) {
+      even[e / 4][e % 4] = (w[2 * e] & 0xffffu) | w[2 * e + 1] << 16;
+      odd[e / 4][e % 4] = w[2 * e] >> 16 | (w[2 * e + 1] & 0xffff0000u);
     }
+    const int s1 = s0 + b - a;
+    put_run(dst, even, s0, s1);
+    put_run(dst + 16, odd, s0, s1);
   }
 }
 
