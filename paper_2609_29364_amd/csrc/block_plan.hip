@@ -75,52 +75,62 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PlanArgs A, int counters
   int a[PER], count[PER], len[PER], own[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) {   // (all the loads in flight)
-    const int r = min(tid * PER + i, n - 1);
+    const int r = min(i * kThreads + tid, n - 1);
     a[i] = n ? A.indptr[r] : 0;
     count[i] = n ? A.indptr[r + 1] : 0;
     len[i] = n ? A.lens[r] : 0;
     own[i] = n ? A.owned[r] : 0;
   }
-  int64_t need[PER], sum = 0;
-  bool wide[PER];   // more tokens than the table's row holds
+  int32_t need[PER];   // -1: more tokens than the table's row holds
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int r = tid * PER + i;
+    const int r = i * kThreads + tid;
     a[i] = min(max(a[i], 0), A.total_q);
     count[i] = min(max(count[i], a[i]), A.total_q) - a[i];
     len[i] = max(len[i], 0);
     own[i] = min(max(own[i], 0), A.width);
     const int64_t blocks = ((int64_t)len[i] + count[i] + NSD_BLOCK_SIZE - 1) / NSD_BLOCK_SIZE;
-    wide[i] = blocks > A.width;
-    need[i] = wide[i] || r >= n ? 0 : max(blocks - own[i], (int64_t)0);
-    sum += need[i];
+    need[i] = blocks > A.width ? -1 : max((int32_t)blocks - own[i], 0);
     if (r < n) {
       indptr[r] = a[i];
       lens[r] = len[i];
+      start[r] = max(need[i], 0);
     }
+  }
+  __syncthreads();
+  // the prefix, each thread PER requests that follow each other
+  int32_t each[PER];
+  int64_t sum = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    each[i] = tid * PER + i < n ? start[tid * PER + i] : 0;
+    sum += each[i];
   }
   int64_t upto = scan(sum, part) - sum;
   int32_t mine = 0;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int r = tid * PER + i;
-    const int64_t before = upto;
-    upto += need[i];
-    const bool ok = !wide[i] && (need[i] == 0 || upto <= free_n);
-    if (r >= n) continue;
     // past the granted requests the prefix stays above every granted block's number
-    start[r] = (int32_t)min(before, (int64_t)free_n);
-    owned[r] = ok ? own[i] : -1;
-    if (ok && need[i]) mine = (int32_t)upto;
-    if (counters && blockIdx.x == 0) {
-      A.granted[r] = ok;
-      A.new_owned[r] = own[i] + (ok ? (int32_t)need[i] : 0);
-      A.new_lens[r] = len[i] + (ok ? count[i] : 0);
-    }
+    if (tid * PER + i < n) start[tid * PER + i] = (int32_t)min(upto, (int64_t)free_n);
+    upto += each[i];
+    if (each[i] && upto <= free_n) mine = (int32_t)upto;
   }
   // the ids taken: up to the last granted request that needs some (the prefix does not fall)
   const uint64_t m = __ballot(mine > 0);
   if ((tid & 63) == (m ? 63 - __builtin_clzll(m) : 0)) taken[tid >> 6] = mine;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int r = i * kThreads + tid;
+    if (r >= n) continue;
+    const bool ok = need[i] == 0 || (need[i] > 0 && (int64_t)start[r] + need[i] <= free_n);
+    owned[r] = ok ? own[i] : -1;
+    if (counters && blockIdx.x == 0) {
+      A.granted[r] = ok;
+      A.new_owned[r] = own[i] + (ok ? need[i] : 0);
+      A.new_lens[r] = len[i] + (ok ? count[i] : 0);
+    }
+  }
   __syncthreads();
   int32_t used = 0;
 #pragma unroll
@@ -166,32 +176,38 @@ __global__ __launch_bounds__(kThreads) void trim_kernel(TrimArgs A, int counters
   const int n = A.bs, tid = threadIdx.x;
   int32_t *start = mem, *kept = mem + (n + 1);
   const int free_n = min(max(A.free_count[0], 0), A.capacity);
-  int32_t own[PER], keep[PER], back[PER];
+  int32_t own[PER], keep[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) {   // (all the loads in flight)
-    const int r = min(tid * PER + i, n - 1);
+    const int r = min(i * kThreads + tid, n - 1);
     own[i] = n ? A.owned[r] : 0;
     keep[i] = n ? A.keep[r] : 0;
   }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int r = i * kThreads + tid, o = min(max(own[i], 0), A.width);
+    const int64_t b = ((int64_t)max(keep[i], 0) + NSD_BLOCK_SIZE - 1) / NSD_BLOCK_SIZE;
+    const int k = (int)min((int64_t)o, b);
+    if (r >= n) continue;
+    start[r] = o - k;
+    kept[r] = k;
+    if (counters && blockIdx.x == 0) A.new_owned[r] = k;
+  }
+  __syncthreads();
+  // the prefix, each thread PER requests that follow each other
+  int32_t each[PER];
   int64_t sum = 0;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int o = min(max(own[i], 0), A.width);
-    const int64_t b = ((int64_t)max(keep[i], 0) + NSD_BLOCK_SIZE - 1) / NSD_BLOCK_SIZE;
-    keep[i] = (int)min((int64_t)o, b);
-    back[i] = tid * PER + i < n ? o - keep[i] : 0;
-    sum += back[i];
+    each[i] = tid * PER + i < n ? start[tid * PER + i] : 0;
+    sum += each[i];
   }
   const int64_t end = scan(sum, part);
   int64_t upto = end - sum;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int r = tid * PER + i;
-    if (r >= n) continue;
-    start[r] = (int32_t)upto;
-    kept[r] = keep[i];
-    upto += back[i];
-    if (counters && blockIdx.x == 0) A.new_owned[r] = keep[i];
+    if (tid * PER + i < n) start[tid * PER + i] = (int32_t)upto;
+    upto += each[i];
   }
   // ids past the list's capacity are dropped
   if (tid == kThreads - 1) total = (int32_t)min(end, (int64_t)(A.capacity - free_n));
@@ -206,7 +222,7 @@ __global__ __launch_bounds__(kThreads) void trim_kernel(TrimArgs A, int counters
 
 // Workgroups for `work` blocks and tokens: one where its threads take at most four each.
 int groups(int64_t work) {
-  const int64_t g = work <= 4 * kThreads ? 1 : (work + 2 * kThreads - 1) / (2 * kThreads);
+  const int64_t g = work <= 4 * kThreads ? 1 : (work + kThreads - 1) / kThreads;
   return (int)(g < 256 ? g : 256);
 }
 
