@@ -706,17 +706,35 @@ const Tensor& typed(PyObject* o, at::ScalarType type, at::Device dev) {
   return t;
 }
 
-// `n` int32 entries; a new tensor (kept by own) where o is None and one may be made.
-int32_t* entries(PyObject* o, int64_t n, const Tensor& like, Tensor* own = nullptr) {
-  if (own && o == Py_None) {
-    *own = at::empty({n}, like.options().dtype(at::kInt));
-    return own->data_ptr<int32_t>();
-  }
+// `n` int32 entries.
+const Tensor& checked_entries(PyObject* o, int64_t n, const Tensor& like) {
   const Tensor& t = typed(o, at::kInt, like.device());
   need(t.numel() == n);
-  if (own) *own = t;
-  return t.data_ptr<int32_t>();
+  return t;
 }
+int32_t* entries(PyObject* o, int64_t n, const Tensor& like) {
+  return checked_entries(o, n, like).data_ptr<int32_t>();
+}
+
+// A call's int32 outputs: the caller's, or parts of one new allocation (an allocation each
+// took longer than the kernel of a small step).
+struct Outputs {
+  const Tensor& like;
+  int64_t left;   // entries of all outputs together
+  Tensor room;
+  int32_t* take(PyObject* o, int64_t n, Tensor* out) {
+    if (o != Py_None) {
+      *out = checked_entries(o, n, like);
+    } else {
+      if (!room.defined()) room = at::empty({left}, like.options().dtype(at::kInt));
+      *out = Tensor(room.unsafeGetTensorImpl()->shallow_copy_and_detach(c10::VariableVersion(0), false));
+      out->unsafeGetTensorImpl()->set_sizes_contiguous({n});
+      out->unsafeGetTensorImpl()->set_storage_offset(room.numel() - left);
+    }
+    left -= n;
+    return out->data_ptr<int32_t>();
+  }
+};
 
 template <int N>
 PyObject* wrap_list(void* t) {
@@ -739,9 +757,10 @@ PyObject* py_plan_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
                   *indptr = entries(a[3], (int64_t)bs + 1, t), *count = entries(a[5], 1, t);
     const int32_t capacity = small(f.numel());
     Tensor out[5];
-    int32_t *o = entries(a[7], bs, t, &out[0]), *l = entries(a[8], bs, t, &out[1]),
-            *c = entries(a[9], 1, t, &out[2]), *g = entries(a[10], bs, t, &out[3]),
-            *s = entries(a[11], total, t, &out[4]);
+    Outputs outs{t, 3 * (int64_t)bs + 1 + total};
+    int32_t *o = outs.take(a[7], bs, &out[0]), *l = outs.take(a[8], bs, &out[1]),
+            *c = outs.take(a[9], 1, &out[2]), *g = outs.take(a[10], bs, &out[3]),
+            *s = outs.take(a[11], total, &out[4]);
     int32_t *table = t.data_ptr<int32_t>(), *ids = f.data_ptr<int32_t>();
     void* stream = stream_of(t);
     return unlocked([&] {
@@ -761,7 +780,8 @@ PyObject* py_trim_blocks(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int32_t *owned = entries(a[1], bs, t), *keep = entries(a[2], bs, t),
                   *count = entries(a[4], 1, t);
     Tensor out[2];
-    int32_t *o = entries(a[5], bs, t, &out[0]), *c = entries(a[6], 1, t, &out[1]);
+    Outputs outs{t, (int64_t)bs + 1};
+    int32_t *o = outs.take(a[5], bs, &out[0]), *c = outs.take(a[6], 1, &out[1]);
     int32_t *table = t.data_ptr<int32_t>(), *ids = f.data_ptr<int32_t>();
     void* stream = stream_of(t);
     return unlocked([&] {
