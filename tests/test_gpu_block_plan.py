@@ -82,6 +82,15 @@ def test_trim(device, bs, width, in_place):
     assert np.array_equal(f.cpu().numpy(), rf) and torch.equal(t, i32(table, device))
 
 
+def test_rows_behind_the_last_request_have_no_slot(device):
+    table, owned, lens, indptr, free, count = make(8, 30, 20, 9, 60, lens_hi=100)
+    rt, ro, rl, rc, rg, rs = prompt.plan_blocks(table, owned, lens, indptr, free, count, indptr[-1])
+    t, o, l, q, f, c = (i32(x, device) for x in (table, owned, lens, indptr, free, [count]))
+    s = nsd.plan_blocks(t, o, l, q, f, c, int(indptr[-1]) + 5000)[4].cpu().numpy()
+    assert np.array_equal(s[:indptr[-1]], rs) and (s[indptr[-1]:] == -1).all()
+    assert np.array_equal(t.cpu().numpy(), rt)
+
+
 def test_a_batch_of_none(device):
     e = torch.empty(0, dtype=torch.int32, device=device)
     c = i32([3], device)

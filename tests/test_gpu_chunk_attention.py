@@ -145,6 +145,50 @@ def test_split_contexts(device, ctx, new):
     b.check(out)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("ctx, new", [([2500], [1]), ([1500, 20], [3, 40]), ([1100, 900, 30], [70, 1, 2])])
+def test_split_contexts_with_masks(device, ctx, new, d):
+    b = Batch(device, ctx, new, 4, 2, d, seed=d)
+    assert nsd.chunk_attention_workspace_size(len(ctx), b.total, 4, 2, d, max(new), max(b.lens)) > 0
+    pos = np.concatenate([np.arange(c, c + n) for c, n in zip(b.ctx, b.new)])
+    b.check(first=np.maximum(pos - 1000, 0), prefix=[70] * len(ctx), softcap=8.0,
+            slopes=[0.5, 0.002, 0.0, 0.01])
+    # a split that sees nothing, and infinities in hidden tokens of others
+    first = np.maximum(pos - 5, 0)
+    b.put(0, 50, k=float("nan"), v=float("inf"))
+    b.put(0, 700, v=float("nan"))
+    b.check(first=first)
+
+
+@pytest.mark.parametrize("bs, hkv, ctx_hi", [(20, 32, 60), (70, 8, 900), (130, 4, 1500), (256, 2, 800),
+                                             (257, 4, 100)])
+def test_batches_placed_by_length(device, bs, hkv, ctx_hi):
+    """Batches whose items are ordered, and split, by the lengths of one to four requests a lane."""
+    rng = np.random.default_rng(bs)
+    ctx = np.where(rng.random(bs) < 0.8, rng.integers(0, 60, bs), rng.integers(0, ctx_hi, bs))
+    new = rng.choice([0, 1, 1, 1, 1, 2, 40], bs)
+    new[rng.integers(bs)] = 130
+    Batch(device, ctx.tolist(), new.tolist(), 2 * hkv, hkv, 64, seed=bs).check()
+
+
+def test_rows_behind_the_last_request_stay(device):
+    b = Batch(device, [30, 500, 2], [20, 1, 7], 4, 2, 64)
+    dev, pad = device, 300
+    q = torch.cat([b.q, torch.randn((pad, 4, 64)).bfloat16()]).to(dev)
+    out = torch.full_like(q, 7.0)
+    nsd.chunk_attention(q, b.k.to(dev), b.v.to(dev), i32(b.table, dev), i32(b.lens, dev),
+                        i32(b.indptr, dev), 20, 501, out=out)
+    b.check(out[:b.total])
+    assert (out[b.total:] == 7).all()
+
+
+def test_a_tiny_cap(device):
+    b = Batch(device, [40], [50], 2, 1, 64)
+    got = b.run(softcap=1e-38).double().cpu().numpy()     # every score is then 0
+    ref, tol = b.ref(scale=0.0)
+    assert (np.abs(got - ref) <= tol).all()
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.2, 1.0, 1e-3])
 def test_scales(device, scale):
     Batch(device, [50, 0], [70, 3], 4, 2, 64).check(scale=scale)
