@@ -212,14 +212,16 @@ __device__ inline Piece find_piece(const Params& P, const int32_t* indptr, const
   int mine = 0;
 #pragma unroll
   for (int i = 0; i < kPerLane; ++i) mine += tiles[i] * splits[i];
-  if (idx >= last_lane(sum_scan(mine))) return Piece{-1, 0, 0, 1, 0, 0};
+  const int pieces = last_lane(sum_scan(mine));
+  if (idx >= pieces) return Piece{-1, 0, 0, 1, 0, 0};
   float most = 0.f, each[kPerLane];
 #pragma unroll
   for (int i = 0; i < kPerLane; ++i) {
     each[i] = (float)stages[i] / splits[i];
     if (tiles[i]) most = fmaxf(most, each[i]);
   }
-  most = last_lane(wave_scan(most, 0.f, larger));
+  // pieces that all run at once are one class
+  most = pieces * P.hkv > kSlots ? last_lane(wave_scan(most, 0.f, larger)) : -1.f;
   const float bounds[6] = {INFINITY, 0.75f * most, 0.5f * most, 0.35f * most, 0.2f * most, -1.f};
   int before = 0;
 #pragma unroll
@@ -639,32 +641,24 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
       q[kk] = __builtin_bit_cast(bf16x8, t);
     }
   }
-  // the wave's first keys at the extremes, and its last position
-  int fmax = mine ? w.first : INT32_MIN, fmin = mine ? w.first : INT32_MAX;
-#pragma unroll
-  for (int s = 1; s < 32; s *= 2) {
-    fmax = max(fmax, __shfl_xor(fmax, s));
-    fmin = min(fmin, __shfl_xor(fmin, s));
+  // the lowest and highest first key of the wave's rows and of the workgroup's (at most 128
+  // query tokens), and the wave's first and last position
+  int fmin = 0, fmax = 0, from = 0, high = 0;
+  if (P.first) {
+    const int j0 = (int)(row0 / P.group), j1 = (int)((row0 + count - 1) / P.group);
+    const int f0 = P.first[a0 + min(j0 + lane, j1)], f1 = P.first[a0 + min(j0 + 64 + lane, j1)];
+    const auto less = [](int x, int y) { return min(x, y); };
+    const auto more = [](int x, int y) { return max(x, y); };
+    fmin = last_lane(wave_scan(mine ? w.first : INT32_MAX, INT32_MAX, less));
+    fmax = last_lane(wave_scan(mine ? w.first : INT32_MIN, INT32_MIN, more));
+    from = max(last_lane(wave_scan(min(f0, f1), INT32_MAX, less)), 0);
+    high = max(last_lane(wave_scan(max(f0, f1), INT32_MIN, more)), 0);
   }
-  fmax = uniform(fmax);
-  fmin = uniform(fmin);
   const int64_t wave_last = min(rows, row0 + (rg + 1) * kWaveRows) - 1;
   const int pmin = min(L - n + (int)((row0 + rg * kWaveRows) / P.group), last);
   const int pmax = wave_last >= row0 + rg * kWaveRows
                        ? min(L - n + (int)(wave_last / P.group), last) : -1;
-  int from = 0, high = 0;   // the workgroup's first keys: the lowest and the highest
-  if (P.first) {
-    int32_t* at = (int32_t*)buf0;
-    if (lane == 0) {
-      at[wave] = fmin;
-      at[kWaves + wave] = fmax;
-    }
-    __syncthreads();
-    from = uniform(max(min(min(at[0], at[1]), min(at[2], at[3])), 0));
-    high = uniform(max(max(at[4], at[5]), max(at[6], at[7])));
-    __syncthreads();
-  }
-  const int low = min(L - n + (int)(row0 / P.group), last);   // its first row's position
+  const int low = min(L - n + (int)(row0 / P.group), last);   // the workgroup's first position
   const int to = min(L - n + (int)((min(rows, row0 + kRows) - 1) / P.group), last) + 1;   // past its last key
   // stages: those of the prefix, then from the first key's on
   const int n1 = (prefix + kStage - 1) / kStage;
@@ -915,10 +909,11 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const Params P) {
   __shared__ float2 meet[kTeams];   // (max, sum)
   const int team = threadIdx.x / kTeam, c = threadIdx.x % kTeam;
   constexpr int kParts = kRows / 32;
+  int4 rec = P.records[blockIdx.x / kParts];   // (the grid is no larger than the records)
   const int units = *P.split_items * P.hkv * kParts;
   for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
   const int g = unit / kParts % P.hkv, part0 = unit % kParts * 32;
-  const int4 rec = P.records[unit / kParts];
+  if (unit != (int)blockIdx.x) rec = P.records[unit / kParts];
   const int splits = rec.x & 0xff, row1 = min(rec.w, part0 + 32);
   if (part0 >= row1) continue;
   const int64_t place = (int64_t)(rec.x >> 8) * P.hkv + g;
@@ -1092,9 +1087,10 @@ extern "C" nsd_status nsd_chunk_attention(
   P.part_ml = (float2*)(P.records + split_items);
   P.part = (float*)(P.part_ml + places * kRows);
   P.max_places = pl.places;
-  // the order matters where the items do not all run at once and differ: among few requests,
-  // or more than find_piece() holds, they start as they come
-  P.parted = pl.places || (bs >= 16 && bs <= kPartedBatch && pl.items * num_kv_heads > kSlots);
+  // The order matters where the items do not all run at once and differ: among few requests,
+  // many rounds, or more requests than find_piece() holds, they start as they come.
+  P.parted = pl.places || (bs >= 16 && bs <= kPartedBatch && pl.items * num_kv_heads > kSlots &&
+                           pl.items * num_kv_heads <= 8 * kSlots);
   P.num_blocks = num_blocks;
   // 0 becomes a factor too small to move a weight, as 0 times a hidden token's -infinity is NaN
   P.scale = std::max(std::fabs(scale) * kLog2e, 1e-37f);
