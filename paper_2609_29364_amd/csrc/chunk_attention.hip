@@ -55,7 +55,6 @@ constexpr int kSlots = 512;                  // workgroups resident on 256 CUs, 
 constexpr int kPerLane = 4;                  // requests a lane looks at where the batch is parted
 constexpr int kPartedBatch = 64 * kPerLane;
 constexpr int kMaxSplits = 64;
-constexpr int kJoinThreads = 1024;
 
 struct Params {
   const uint16_t* q;
@@ -900,82 +899,77 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
   if (lane < 32) P.part_ml[at] = make_float2(a.m, l);
 }
 
-// The splits of an item's rows joined, 32 rows at a time: D/4 threads take a row's columns,
-// several such teams part many splits and meet in LDS.
+// The splits of an item's rows joined (blockIdx.x: the item and KV head): D/4 threads take a
+// row's columns, several such teams part many splits and meet in LDS.  A few rows of 64
+// splits are many loads after one another, so an item's rows are spread over gridDim.y.
 template <int D>
-__global__ __launch_bounds__(kJoinThreads) void join_kernel(const Params P) {
-  constexpr int kTeam = D / 4, kTeams = kJoinThreads / kTeam;
+__global__ __launch_bounds__(kThreads) void join_kernel(const Params P) {
+  constexpr int kTeam = D / 4, kTeams = kThreads / kTeam;
   __shared__ float4 sums[kTeams][kTeam];
   __shared__ float2 meet[kTeams];   // (max, sum)
-  const int team = threadIdx.x / kTeam, c = threadIdx.x % kTeam;
-  constexpr int kParts = kRows / 32;
-  int4 rec = P.records[blockIdx.x / kParts];   // (the grid is no larger than the records)
-  const int units = *P.split_items * P.hkv * kParts;
-  for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
-  const int g = unit / kParts % P.hkv, part0 = unit % kParts * 32;
-  if (unit != (int)blockIdx.x) rec = P.records[unit / kParts];
-  const int splits = rec.x & 0xff, row1 = min(rec.w, part0 + 32);
-  if (part0 >= row1) continue;
+  const int team = threadIdx.x / kTeam, c = threadIdx.x % kTeam, g = blockIdx.x % P.hkv;
+  const int4 rec = P.records[blockIdx.x];
+  if ((int)(blockIdx.x / P.hkv) >= *P.split_items) return;
+  const int splits = rec.x & 0xff, count = rec.w;
   const int64_t place = (int64_t)(rec.x >> 8) * P.hkv + g;
-  const int teams = splits > 16 ? 8 : splits > 8 ? 4 : splits > 4 ? 2 : 1;
+  const int teams = splits > 16 ? 8 : splits > 8 ? 4 : splits > 4 ? 2 : 1, rows = kTeams / teams;
   const int first = team & (teams - 1);
-  for (int row0 = part0; row0 < row1; row0 += kTeams / teams) {
-  const int row = row0 + team / teams;
-  const bool in = row < row1;
-  const int64_t at = place * kRows + row, step = (int64_t)P.hkv * kRows;
-  float m = -INFINITY, sum = 0.f;
-  float4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = first; in && s0 < splits; s0 += 4 * teams) {
-    float2 x[4];
-    float4 y[4];
+  for (int row0 = blockIdx.y * rows; row0 < count; row0 += gridDim.y * rows) {
+    const int row = row0 + team / teams;
+    const bool in = row < count;
+    const int64_t at = place * kRows + row, step = (int64_t)P.hkv * kRows;
+    float m = -INFINITY, sum = 0.f;
+    float4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = first; in && s0 < splits; s0 += 4 * teams) {
+      float2 x[4];
+      float4 y[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {   // the four loads in flight; past the last split: nothing seen
-      const int s = min(s0 + u * teams, splits - 1);
-      x[u] = P.part_ml[at + s * step];
-      y[u] = *(const float4*)(P.part + (at + s * step) * D + c * 4);
-      if (s0 + u * teams >= splits || x[u].y == 0.f) x[u] = make_float2(-INFINITY, 0.f);
-    }
-    const float top = fmaxf(fmaxf(m, fmaxf(x[0].x, x[1].x)), fmaxf(x[2].x, x[3].x));
-    const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-    m = top;
-    sum *= keep;
-    o.x *= keep, o.y *= keep, o.z *= keep, o.w *= keep;
+      for (int u = 0; u < 4; ++u) {   // the four loads in flight; past the last split: nothing seen
+        const int s = min(s0 + u * teams, splits - 1);
+        x[u] = P.part_ml[at + s * step];
+        y[u] = *(const float4*)(P.part + (at + s * step) * D + c * 4);
+        if (s0 + u * teams >= splits || x[u].y == 0.f) x[u] = make_float2(-INFINITY, 0.f);
+      }
+      const float top = fmaxf(fmaxf(m, fmaxf(x[0].x, x[1].x)), fmaxf(x[2].x, x[3].x));
+      const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+      m = top;
+      sum *= keep;
+      o.x *= keep, o.y *= keep, o.z *= keep, o.w *= keep;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      if (x[u].y == 0.f) continue;
-      const float f = __builtin_amdgcn_exp2f(x[u].x - m) * x[u].y;
-      sum += f;
-      o.x += f * y[u].x, o.y += f * y[u].y, o.z += f * y[u].z, o.w += f * y[u].w;
+      for (int u = 0; u < 4; ++u) {
+        if (x[u].y == 0.f) continue;
+        const float f = __builtin_amdgcn_exp2f(x[u].x - m) * x[u].y;
+        sum += f;
+        o.x += f * y[u].x, o.y += f * y[u].y, o.z += f * y[u].z, o.w += f * y[u].w;
+      }
     }
-  }
-  if (teams > 1) {
-    __syncthreads();
-    sums[team][c] = o;
-    if (c == 0) meet[team] = make_float2(m, sum);
-    __syncthreads();
-    float top = m;
-    for (int t = 1; t < teams; ++t) top = fmaxf(top, meet[team - first + t].x);
-    const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-    sum *= keep;
-    o.x *= keep, o.y *= keep, o.z *= keep, o.w *= keep;
-    for (int t = 1; t < teams; ++t) {
-      const float2 x = meet[team - first + t];
-      if (x.x == -INFINITY) continue;
-      const float f = __builtin_amdgcn_exp2f(x.x - top);
-      const float4 y = sums[team - first + t][c];
-      sum += f * x.y;
-      o.x += f * y.x, o.y += f * y.y, o.z += f * y.z, o.w += f * y.w;
+    if (teams > 1) {
+      __syncthreads();
+      sums[team][c] = o;
+      if (c == 0) meet[team] = make_float2(m, sum);
+      __syncthreads();
+      float top = m;
+      for (int t = 1; t < teams; ++t) top = fmaxf(top, meet[team - first + t].x);
+      const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+      sum *= keep;
+      o.x *= keep, o.y *= keep, o.z *= keep, o.w *= keep;
+      for (int t = 1; t < teams; ++t) {
+        const float2 x = meet[team - first + t];
+        if (x.x == -INFINITY) continue;
+        const float f = __builtin_amdgcn_exp2f(x.x - top);
+        const float4 y = sums[team - first + t][c];
+        sum += f * x.y;
+        o.x += f * y.x, o.y += f * y.y, o.z += f * y.z, o.w += f * y.w;
+      }
     }
-  }
-  if (in && first == 0) {
-    const float f = sum == 0.f ? 0.f : 1.f / sum;
-    const int r = rec.z + row, j = r / P.group, h = r - j * P.group;
-    u32x2 y;
-    y[0] = pack(o.x * f, o.y * f);
-    y[1] = pack(o.z * f, o.w * f);
-    *(u32x2*)(P.out + ((int64_t)(rec.y + j) * P.hq + g * P.group + h) * D + c * 4) = y;
-  }
-  }
+    if (in && first == 0) {
+      const float f = sum == 0.f ? 0.f : 1.f / sum;
+      const int r = rec.z + row, j = r / P.group, h = r - j * P.group;
+      u32x2 y;
+      y[0] = pack(o.x * f, o.y * f);
+      y[1] = pack(o.z * f, o.w * f);
+      *(u32x2*)(P.out + ((int64_t)(rec.y + j) * P.hq + g * P.group + h) * D + c * 4) = y;
+    }
   }
 }
 
@@ -1119,12 +1113,13 @@ extern "C" nsd_status nsd_chunk_attention(
   }
   if (const nsd_status st = check_launch(fn)) return st;
   if (pl.places) {
-    // at most a workgroup a CU, each taking several items' rows in turn
-    const dim3 grid((uint32_t)std::min<int64_t>(split_items * (kRows / 32), kSlots / 2));
+    // about four workgroups a CU
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(32, 1024 / split_items));
+    const dim3 grid((uint32_t)split_items, (uint32_t)parts);
     if (head_dim == 64)
-      hipLaunchKernelGGL(join_kernel<64>, grid, dim3(kJoinThreads), 0, (hipStream_t)stream, P);
+      hipLaunchKernelGGL(join_kernel<64>, grid, dim3(kThreads), 0, (hipStream_t)stream, P);
     else
-      hipLaunchKernelGGL(join_kernel<128>, grid, dim3(kJoinThreads), 0, (hipStream_t)stream, P);
+      hipLaunchKernelGGL(join_kernel<128>, grid, dim3(kThreads), 0, (hipStream_t)stream, P);
     return check_launch(fn);
   }
   return NSD_OK;
