@@ -139,6 +139,7 @@ __device__ inline int sum_scan(int x) { return wave_scan(x, 0, [](int a, int b) 
 // place: of its partial result; record: of its item.  r < 0: nothing.
 struct Piece {
   int r, tile, split, splits, place, record;
+  int a0, a1, length;   // the request's query rows; its length, at most max_len
 };
 
 // The idx-th piece of a batch of at most kPartedBatch requests, found by every wave from the
@@ -212,7 +213,7 @@ __device__ inline Piece find_piece(const Params& P, const int32_t* indptr, const
 #pragma unroll
   for (int i = 0; i < kPerLane; ++i) mine += tiles[i] * splits[i];
   const int pieces = last_lane(sum_scan(mine));
-  if (idx >= pieces) return Piece{-1, 0, 0, 1, 0, 0};
+  if (idx >= pieces) return Piece{-1};
   float most = 0.f, each[kPerLane];
 #pragma unroll
   for (int i = 0; i < kPerLane; ++i) {
@@ -242,11 +243,14 @@ __device__ inline Piece find_piece(const Params& P, const int32_t* indptr, const
         p.tile = t - 1 - local / n;   // a request's last rows see the most tokens
         p.place = n > 1 ? at(base[i]) + p.tile * n + p.split : 0;
         p.record = n > 1 ? at(nth[i]) + p.tile : 0;
+        p.a0 = at(a[i]);
+        p.a1 = at(b[i]);
+        p.length = min(max(at(L[i]), 0), P.max_len);
         return p;
       }
       before = last_lane(upto);
     }
-  return Piece{-1, 0, 0, 1, 0, 0};
+  return Piece{-1};
 }
 
 // 1 KiB from src + OFFSET to dst + OFFSET, 16 bytes a lane.
@@ -600,16 +604,16 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
     const int item = P.items - 1 - x / P.hkv;
     const int r = find_request(P, indptr, item);
     piece = Piece{r, item - first_item(P, indptr, r), 0, 1, 0, 0};
+    piece.a0 = min(max(indptr[r], 0), P.total_q);
+    piece.a1 = min(max(indptr[r + 1], piece.a0), P.total_q);
+    piece.length = min(max(lens[r], 0), P.max_len);
   }
   const int r = piece.r;
-  const int a0 = min(max(indptr[r], 0), P.total_q);
-  const int a1 = min(max(indptr[r + 1], a0), P.total_q);
-  const int n = a1 - a0;
+  const int a0 = piece.a0, n = piece.a1 - a0;
   const int64_t rows = (int64_t)n * P.group;
   const int64_t row0 = (int64_t)piece.tile * kRows;
   if (row0 < 0 || row0 >= rows) return;
-  const int L = min(max(lens[r], 0),
-                    min(P.max_len, P.width < (1 << 26) ? P.width * 16 : 1 << 30));
+  const int L = min(piece.length, P.width < (1 << 26) ? P.width * 16 : 1 << 30);
   const int last = L - 1;
   const int prefix = prefixes ? min(max(prefixes[r], 0), L) : 0;
 
@@ -1081,9 +1085,9 @@ extern "C" nsd_status nsd_chunk_attention(
   P.part_ml = (float2*)(P.records + split_items);
   P.part = (float*)(P.part_ml + places * kRows);
   P.max_places = pl.places;
-  // The order matters where the items do not all run at once and differ: among few requests,
+  // The order matters where the items do not all run at once and differ: of few or short requests,
   // many rounds, or more requests than find_piece() holds, they start as they come.
-  P.parted = pl.places || (bs >= 16 && bs <= kPartedBatch && pl.items * num_kv_heads > kSlots &&
+  P.parted = pl.places || (max_seq_len > 12 * kStage && bs >= 16 && bs <= kPartedBatch && pl.items * num_kv_heads > kSlots &&
                            pl.items * num_kv_heads <= 8 * kSlots);
   P.num_blocks = num_blocks;
   // 0 becomes a factor too small to move a weight, as 0 times a hidden token's -infinity is NaN
