@@ -20,6 +20,11 @@
 // block.  A run is at most 16 rows; the workgroup whose rows hold its first row takes all of
 // it.  Slots that a run does not fill are not touched (narrower stores), so rows may name slots
 // in any order.
+//
+// Measured (head_dim 128): 15555 rows of 32/8 heads, three axes, 383 MB, 76-90 us, the rate of a
+// copy; 1280 rows in windows of 5 15 us, 8 of them the stores of partial sectors (a run as
+// pairs, fours and eights of slots 14.8 us, slot by slot 17.7); 64 single rows of 16/8 heads 4.1
+// us (all kinds in one workgroup, one after the other, 9.9).
 #include "nsd_internal.h"
 
 #include <algorithm>
@@ -374,7 +379,7 @@ extern "C" nsd_status nsd_rope_append(void* k_pool, void* v_pool, int64_t num_bl
   A.hkv = num_kv_heads;
   A.rot = rot_dim;
   // Few rows: few of them a workgroup, and a workgroup for each group of heads, until the device
-  // has enough workgroups.
+  // has enough workgroups (four a CU).
   A.rows = total_q <= 256 ? 4 : kRows;
   const int64_t tiles = ((int64_t)total_q + A.rows - 1) / A.rows;
   int64_t blocks = 0;
