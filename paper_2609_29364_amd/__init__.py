@@ -647,6 +647,7 @@ def plan_blocks(block_table, owned, seq_lens, q_indptr, free_blocks, free_count,
     new_lens = _i32s(bs, "new_lens", new_lens, owned)
     new_free_count = _i32s(1, "new_free_count", new_free_count, owned)
     granted = _i32s(bs, "granted", granted, owned)
+    total_q = int(total_q)
     if total_q < 0:
         raise ValueError("total_q must not be negative")
     slots = _i32s(total_q, "slots", slots, owned)
@@ -790,6 +791,7 @@ def chunk_attention(q, k_cache, v_cache, block_table, seq_lens, q_indptr, max_q_
     _dev(v_cache, torch.bfloat16, "v_cache")
     if q.dim() != 3 or k_cache.dim() != 5:
         raise ValueError("q must be [total_q][Hq][D], k_cache [blocks][Hkv][D/8][16][8]")
+    max_q_per_seq, max_seq_len = int(max_q_per_seq), int(max_seq_len)
     total_q, hq, d = q.shape
     nb, hkv, dv8, bsz, vec = k_cache.shape
     if dv8 * vec != d or vec != 8 or v_cache.shape != (nb, hkv, d, bsz):

@@ -87,6 +87,17 @@ def test_chunks_and_single_tokens(device):
         assert np.abs(got[r:r + 1] - ref).max() <= 0.05
 
 
+def test_without_the_marshalling_module(device, monkeypatch):
+    """The same steps through ctypes, with numpy integers among the arguments."""
+    monkeypatch.setattr(nsd, "_native_module", nsd._NoBinding())
+    w = Worker(device, 3)
+    w.step(np.array([50, 1, 0]))
+    w.step(np.array([1, 1, 100]))
+    nsd.trim_blocks(w.table, w.owned, w.lens, w.free, w.count, new_owned=w.owned,
+                    new_free_count=w.count)
+    w.step([1, 1, 1], softcap=10.0)
+
+
 def test_a_pool_that_runs_short(device):
     w = Worker(device, 3)
     w.step([500, 300, 100])                       # 32 + 19 + 7 of 64 blocks
