@@ -55,7 +55,7 @@ constexpr int kMaxBatch = 8192;
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kWaveRows = 32;
-constexpr int kRows = kWaves * kWaveRows;    // query rows (token, head of the group) of an item
+constexpr int kRows = kWaves * kWaveRows;    // query rows (token, head of the group) of an item, at most
 constexpr int kStage = 64;                   // tokens of a stage
 constexpr int kStageBlocks = kStage / NSD_BLOCK_SIZE;
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -81,7 +81,7 @@ struct Params {
   int64_t num_blocks;
   float scale, cap;   // scale log2 e > 0 (a negative scale's sign is in `negate`)
   uint32_t negate;    // 0x80008000: Q's signs are flipped
-  int32_t width, bs, total_q, hq, hkv, group, max_len, items, max_places, parted;
+  int32_t width, bs, total_q, hq, hkv, group, max_len, tile, items, max_places, parted;
 };
 
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -99,10 +99,10 @@ __device__ inline float other_half(float x) {
 }
 
 // The first item of request r: its rows' tiles are items first_item(r) .. first_item(r + 1) - 1,
-// which are at least ceil(rows / kRows) of them whatever the rows, so no prefix sum is needed.
+// which are at least ceil(rows / tile) of them whatever the rows, so no prefix sum is needed.
 __device__ inline int first_item(const Params& P, const int32_t* indptr, int r) {
   const int64_t a = min(max(indptr[r], 0), P.total_q);
-  return (int)(a * P.group / kRows) + r;
+  return (int)(a * P.group / P.tile) + r;
 }
 
 // The last request whose first item is at most `item`, by 64 lanes' probes a round.
@@ -186,7 +186,7 @@ __device__ inline Piece find_piece(const Params& P, const int32_t* indptr, const
     const int length = min(max(L[i], 0), P.max_len);
     const int from = min(max(first[i], 0), length);
     const int seen = min(max(prefix[i], 0), from);
-    tiles[i] = in ? (int)(((int64_t)(b[i] - a[i]) * P.group + kRows - 1) / kRows) : 0;
+    tiles[i] = in ? (int)(((int64_t)(b[i] - a[i]) * P.group + P.tile - 1) / P.tile) : 0;
     stages[i] = in ? max((length - from + seen + kStage - 1) / kStage, 1) : 0;
     splits[i] = 1;
     cost += (float)tiles[i] * stages[i];
@@ -624,20 +624,20 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
   const int r = piece.r;
   const int a0 = piece.a0, n = piece.a1 - a0;
   const int64_t rows = (int64_t)n * P.group;
-  const int64_t row0 = (int64_t)piece.tile * kRows;
+  const int64_t row0 = (int64_t)piece.tile * P.tile;
   if (row0 < 0 || row0 >= rows) return;
   const int L = min(piece.length, P.width < (1 << 26) ? P.width * 16 : 1 << 30);
   const int last = L - 1;
   const int prefix = prefixes ? min(max(prefixes[r], 0), L) : 0;
 
   // few rows: the waves share them (one or two groups of 32) and part the tokens
-  const int count = (int)min(rows - row0, (int64_t)kRows);
+  const int count = (int)min(rows - row0, (int64_t)P.tile);
   const int rgroups = count <= kWaveRows ? 1 : count <= 2 * kWaveRows ? 2 : kWaves;
   const int rg = wave & (rgroups - 1), tgroups = kWaves / rgroups, tg = wave / rgroups;
 
   // this lane's row
   const int64_t row = row0 + rg * kWaveRows + (lane & 31);
-  const bool mine = row < rows;
+  const bool mine = row < row0 + count;
   const int j = mine ? (int)(row / P.group) : 0, h = mine ? (int)(row - (int64_t)j * P.group) : 0;
   Sight w;
   w.p = mine ? min(L - n + j, last) : -1;
@@ -670,12 +670,12 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
     from = max(last_lane(wave_scan(min(f0, f1), INT32_MAX, less)), 0);
     high = max(last_lane(wave_scan(max(f0, f1), INT32_MIN, more)), 0);
   }
-  const int64_t wave_last = min(rows, row0 + (rg + 1) * kWaveRows) - 1;
+  const int64_t wave_last = min(row0 + count, row0 + (rg + 1) * kWaveRows) - 1;
   const int pmin = min(L - n + (int)((row0 + rg * kWaveRows) / P.group), last);
   const int pmax = wave_last >= row0 + rg * kWaveRows
                        ? min(L - n + (int)(wave_last / P.group), last) : -1;
   const int low = min(L - n + (int)(row0 / P.group), last);   // the workgroup's first position
-  const int to = min(L - n + (int)((min(rows, row0 + kRows) - 1) / P.group), last) + 1;   // past its last key
+  const int to = min(L - n + (int)((row0 + count - 1) / P.group), last) + 1;   // past its last key
   // stages: those of the prefix, then from the first key's on
   const int n1 = (prefix + kStage - 1) / kStage;
   const int s2 = max(n1, from / kStage);
@@ -818,7 +818,9 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
         find(next);
         keys();
       }
-      weigh<D, CAP, BIAS, 1>(a, s, [&](int b, int t) { return vr[b][t]; }, P, w, t0, ok, true);
+      const bool all = ((t0 + 31 <= pmin) & (t0 >= fmax)) | (t0 + 32 <= prefix);
+      weigh<D, CAP, BIAS, 1>(a, s, [&](int b, int t) { return vr[b][t]; }, P, w, t0, ok,
+                             !(all & (ok == 3)));
       if (next < j1) values();
       j = next;
     }
@@ -992,17 +994,26 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Params P) {
 
 // Bounds per KV head: a batch's items, the split ones of them and their parts.
 struct Plan {
+  int tile;        // rows of an item
   int64_t items;
   int split_items, places;
 };
 
 Plan plan(int32_t bs, int32_t total_q, int32_t hq, int32_t hkv, int32_t max_len) {
   Plan p;
-  p.items = (int64_t)total_q * (hq / hkv) / kRows + bs;
+  const int64_t stages = ((int64_t)max_len + kStage - 1) / kStage;
+  // Where items of 32 or 64 rows still run all at once, their waves part the tokens of short
+  // contexts: up to 2048 tokens that is faster than 128 rows after one another (512 tokens of a
+  // new request 15.5 -> 13.1 us, four of 350-900 at head_dim 64 20.1 -> 13.6), beyond it the
+  // planes are read too often (512 after 8000 88 -> 131 us).
+  p.tile = kRows;
+  while (stages <= 32 && p.tile > kWaveRows &&
+         ((int64_t)total_q * (hq / hkv) / (p.tile / 2) + bs) * hkv <= kSlots)
+    p.tile /= 2;
+  p.items = (int64_t)total_q * (hq / hkv) / p.tile + bs;
   // The second launch does not pay for itself where the items make two rounds or more of
   // contexts to 8192 tokens (packed documents, 4 requests to 6000 tokens: 105 us without, 122
   // with it), nor where all are short; one much longer item among many does.
-  const int64_t stages = ((int64_t)max_len + kStage - 1) / kStage;
   p.split_items = p.places = 0;
   if (bs > kPartedBatch || stages <= (p.items * hkv > 2 * kSlots ? 129 : 12)) return p;
   // A tile of s stages has at most 1 + s / limit <= 2 s / limit parts if it is split, and the
@@ -1114,6 +1125,7 @@ extern "C" nsd_status nsd_chunk_attention(
   P.hkv = num_kv_heads;
   P.group = num_q_heads / num_kv_heads;
   P.max_len = num_blocks ? max_seq_len : 0;   // without a pool nothing is visible
+  P.tile = pl.tile;
   P.items = (int32_t)pl.items;
   clear_stale_error();
   auto go = [&](auto kernel) {

@@ -15,6 +15,8 @@ from oracle import prompt
 from parity import i32
 
 pytestmark = pytest.mark.gpu
+LONG = 5000     # a bound of the lengths for which items have 128 rows
+both_sizes = pytest.mark.parametrize("bound", [0, LONG])
 
 
 class Batch:
@@ -58,7 +60,9 @@ class Batch:
             self.kv[r][1][t] = v
             self.v[b, :, :, t % 16] = self.kv[r][1][t]
 
-    def run(self, first=None, prefix=None, slopes=None, **kw):
+    def run(self, first=None, prefix=None, slopes=None, bound=0, **kw):
+        """bound: max_seq_len at least; a long one has items of 128 rows, which a short batch's
+        own lengths would not."""
         dev = self.dev
         kw = dict(kw, first_keys=None if first is None else i32(first, dev),
                   prefix_lens=None if prefix is None else i32(prefix, dev),
@@ -67,7 +71,7 @@ class Batch:
         out = torch.full(self.q.shape, 7.0, dtype=torch.bfloat16, device=dev)
         return nsd.chunk_attention(self.q.to(dev), self.k.to(dev), self.v.to(dev),
                                    i32(self.table, dev), i32(self.lens, dev), i32(self.indptr, dev),
-                                   max(1, *self.new), max(1, *self.lens), out=out, **kw)
+                                   max(1, *self.new), max(1, bound, *self.lens), out=out, **kw)
 
     def ref(self, scale=None, softcap=0.0, slopes=None, first=None, prefix=None, valid=None):
         """(outputs, bounds), [total_q][Hq][D]."""
@@ -91,15 +95,17 @@ class Batch:
     def check(self, got=None, rows=None, **kw):
         if got is None:
             valid = kw.pop("valid", None)
-            got = self.run(**kw)
+            got = [self.run(**kw), self.run(bound=LONG, **kw)]
             kw["valid"] = valid
         ref, tol = self.ref(**kw)
-        got = got.double().cpu().numpy()
         rows = slice(None) if rows is None else rows
-        err = np.abs(got - ref)
-        assert np.isfinite(got[rows]).all()
-        assert (err[rows] <= tol[rows]).all(), \
-            f"{float((err - tol)[rows].max())} past the bound, rows {np.unique(np.argwhere(err > tol)[:, 0])[:9]}"
+        for x in got if isinstance(got, list) else [got]:
+            x = x.double().cpu().numpy()
+            with np.errstate(invalid="ignore"):
+                err = np.abs(x - ref)
+            assert np.isfinite(x[rows]).all()
+            assert (err[rows] <= tol[rows]).all(), \
+                f"{float((err - tol)[rows].max())} past the bound, rows {np.unique(np.argwhere(err > tol)[:, 0])[:9]}"
 
 
 @pytest.mark.parametrize("hq, hkv, d", [(4, 2, 64), (32, 8, 128), (16, 8, 128), (8, 8, 64), (5, 1, 128),
@@ -143,6 +149,14 @@ def test_split_contexts(device, ctx, new):
     out = nsd.chunk_attention(b.q.to(dev), b.k.to(dev), b.v.to(dev), i32(b.table, dev),
                               i32(b.lens, dev), i32(b.indptr, dev), max(new), 100000)
     b.check(out)
+
+
+@pytest.mark.parametrize("options", [{}, dict(softcap=20.0, slopes=[0.5, 0.01, 0.0, 0.002] * 2)])
+def test_long_chunks(device, options):
+    b = Batch(device, [3000, 1200, 40], [300, 129, 1], 8, 2, 128)
+    b.check(**options)
+    pos = np.concatenate([np.arange(c, c + n) for c, n in zip(b.ctx, b.new)])
+    b.check(first=np.maximum(pos - 700, 0), prefix=[200, 0, 3], **options)
 
 
 @pytest.mark.parametrize("d", [64, 128])
@@ -235,24 +249,26 @@ def test_prefixes_ahead_of_their_queries(device):
     b.check(got, prefix=[100, 150, 0, 1])
 
 
-def test_rows_that_see_nothing(device):
+@both_sizes
+def test_rows_that_see_nothing(device, bound):
     b = Batch(device, [0, 100, 50], [80, 3, 70], 4, 2, 128)
     first = np.full(b.total, 0)
     first[5:60] = 10**6
     first[83:100] = 2**31 - 1
     first[100:110] = -2**31
-    got = b.run(first=first)
+    got = b.run(first=first, bound=bound)
     b.check(got, first=first)
     assert (got[5:60] == 0).all() and (got[83:100] == 0).all()
     # nothing at all for whole workgroups
-    assert (b.run(first=np.full(b.total, 10**6)) == 0).all()
+    assert (b.run(first=np.full(b.total, 10**6), bound=bound) == 0).all()
 
 
-def test_lengths_shorter_than_the_new_tokens(device):
+@both_sizes
+def test_lengths_shorter_than_the_new_tokens(device, bound):
     b = Batch(device, [0, 0], [90, 20], 4, 2, 64)
     b.lens = [50, 0]
     b.kv = [[x[:50] for x in b.kv[0]], [x[:1] for x in b.kv[1]]]
-    got = b.run()
+    got = b.run(bound=bound)
     ref, tol = prompt.chunk_attention_request(
         b.q[:90].double().numpy(), *(x.double().numpy() for x in b.kv[0]), 50, 0.125), 0.05
     assert (got[:40] == 0).all() and (got[90:] == 0).all()
@@ -276,7 +292,8 @@ def test_infinities_and_nan_in_hidden_tokens(device, value, what):
     b.check(first=first, rows=rows)
 
 
-def test_infinite_values_reach_the_rows_that_see_them(device):
+@both_sizes
+def test_infinite_values_reach_the_rows_that_see_them(device, bound):
     b = Batch(device, [10], [60], 2, 1, 64)
     inf, nan = float("inf"), float("nan")
     v = b.kv[0][1]
@@ -284,7 +301,7 @@ def test_infinite_values_reach_the_rows_that_see_them(device):
         row = v[t].clone()
         row[0, dim] = x
         b.put(0, t, v=row)
-    got = b.run().float().cpu()
+    got = b.run(bound=bound).float().cpu()
     at = lambda p, dim: got[p - 10, 0, dim]
     assert torch.isfinite(got[:20]).all()
     assert at(30, 3) == inf and at(32, 3) == inf and torch.isnan(at(33, 3)) and torch.isnan(at(69, 3))
@@ -302,8 +319,8 @@ def test_blocks_that_cannot_be_read(device):
     b.check(valid=valid)
     # a request none of whose blocks is valid, and a pool without blocks
     b.table[1] = -1
-    got = b.run()
-    assert (got[40:90] == 0).all()
+    for bound in (0, LONG):
+        assert (b.run(bound=bound)[40:90] == 0).all()
     e = torch.empty((0, 2, 8, 16, 8), dtype=torch.bfloat16, device=device)
     out = nsd.chunk_attention(b.q.to(device), e, e.view(0, 2, 64, 16), i32(b.table, device),
                               i32(b.lens, device), i32(b.indptr, device), 50, 400)
@@ -321,15 +338,21 @@ def test_offsets_and_lengths_out_of_range_stay_in_bounds(device):
                             i32(wild(70), device), i32(wild(71), device), 2, 64,
                             first_keys=i32(wild(b.total), device),
                             prefix_lens=i32(wild(70), device), out=room[8:-8])
+        nsd.chunk_attention(b.q.to(device), b.k.nan_to_num().to(device),
+                            b.v.nan_to_num().to(device), i32(wild(b.table.shape), device),
+                            i32(wild(70), device), i32(wild(71), device), 2, LONG,
+                            first_keys=i32(wild(b.total), device),
+                            prefix_lens=i32(wild(70), device), out=room[8:-8])
         assert (room[:8] == 7).all() and (room[-8:] == 7).all()
 
 
-def test_large_scores(device):
+@both_sizes
+def test_large_scores(device, bound):
     """Scores of some thousand, growing along the context: the maximum moves on and on."""
     b = Batch(device, [500], [33], 2, 1, 128)
     for t in range(533):
         b.put(0, t, k=b.kv[0][0][t] * (1 + t / 8))
-    got = b.run(scale=1.0).double().cpu().numpy()
+    got = b.run(scale=1.0, bound=bound).double().cpu().numpy()
     ref, _ = b.ref(scale=1.0)
     # the weights' exponents carry 2^-24 of scores up to about 3e3 in each of some roundings
     size = np.abs(b.kv[0][1].double().numpy()).max()
