@@ -64,6 +64,7 @@ constexpr int kSlots = 512;                  // workgroups resident on 256 CUs, 
 constexpr int kPerLane = 4;                  // requests a lane looks at where the batch is parted
 constexpr int kPartedBatch = 64 * kPerLane;
 constexpr int kMaxSplits = 64;
+constexpr int kUnits = 32;                   // of an item's rows, at most, in the join
 
 struct Params {
   const uint16_t* q;
@@ -81,7 +82,7 @@ struct Params {
   int64_t num_blocks;
   float scale, cap;   // scale log2 e > 0 (a negative scale's sign is in `negate`)
   uint32_t negate;    // 0x80008000: Q's signs are flipped
-  int32_t width, bs, total_q, hq, hkv, group, max_len, tile, items, max_places, parted;
+  int32_t width, bs, total_q, hq, hkv, group, max_len, tile, items, max_places, parted, units;
 };
 
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -157,8 +158,9 @@ struct Piece {
 // A tile's cost is the stages its request's tokens span.  A slot's fair share of the batch is
 // total / (kSlots / hkv).  Where the tiles are fewer than the slots, they are split so that all
 // pieces run in one round; where they are more, only a tile of more than 1.5 shares is (a part
-// costs its rows' partial results, written and read).  Long pieces go first, in five classes of
-// length.  All waves compute the same from the same lengths.
+// costs its rows' partial results, written and read), or, if there is none, those that would
+// begin a last round less than half full.  Long pieces go first, in five classes of length.
+// All waves compute the same from the same lengths.
 __device__ inline Piece find_piece(const Params& P, const int32_t* indptr, const int32_t* lens,
                                    const int32_t* prefixes, int idx) {
   const int lane = threadIdx.x & 63, per = (P.bs + 63) / 64;
@@ -196,6 +198,7 @@ __device__ inline Piece find_piece(const Params& P, const int32_t* indptr, const
   const auto larger = [](float x, float y) { return fmaxf(x, y); };
   const float total = last_lane(wave_scan(cost, 0.f, add));
   const int items = last_lane(sum_scan(count));
+  int tail = 0, tail_splits = 1;
   if (P.max_places) {
     const float slots = (float)kSlots / P.hkv;
     const float limit = fmaxf(items < slots ? total / (slots - 0.5f * items) : 1.5f * total / slots, 4.f);
@@ -216,13 +219,23 @@ __device__ inline Piece find_piece(const Params& P, const int32_t* indptr, const
       for (int i = 0; i < kPerLane; ++i) splits[i] = 1;
       split_items = 0;
     }
+    const int round = kSlots / P.hkv, over = round ? items % round : 0;
+    if (split_items == 0 && items > round && over > 0 && 2 * over <= round) {
+      // two ragged chunks (194 tiles a head) 2897 -> 2530 us, 8300 tokens after 24000 3712 -> 3400
+      tail = over;
+      tail_splits = min(round / over, 16);
+      split_items = tail;
+    }
     if (blockIdx.x == 0 && threadIdx.x == 0) *P.split_items = split_items;
   }
   int mine = 0;
 #pragma unroll
   for (int i = 0; i < kPerLane; ++i) mine += tiles[i] * splits[i];
-  const int pieces = last_lane(sum_scan(mine));
+  const int whole = last_lane(sum_scan(mine)) - tail, pieces = whole + tail * tail_splits;
   if (idx >= pieces) return Piece{-1};
+  const int part = idx < whole ? 0 : (idx - whole) % tail_splits;
+  const int nth_tail = idx < whole ? -1 : (idx - whole) / tail_splits;
+  if (nth_tail >= 0) idx = whole + nth_tail;
   float most = 0.f, each[kPerLane];
 #pragma unroll
   for (int i = 0; i < kPerLane; ++i) {
@@ -252,6 +265,12 @@ __device__ inline Piece find_piece(const Params& P, const int32_t* indptr, const
         p.tile = t - 1 - local / n;   // a request's last rows see the most tokens
         p.place = n > 1 ? at(base[i]) + p.tile * n + p.split : 0;
         p.record = n > 1 ? at(nth[i]) + p.tile : 0;
+        if (nth_tail >= 0) {   // (no request is split besides)
+          p.splits = tail_splits;
+          p.split = part;
+          p.place = nth_tail * tail_splits + part;
+          p.record = nth_tail;
+        }
         p.a0 = at(a[i]);
         p.a1 = at(b[i]);
         p.length = min(max(at(L[i]), 0), P.max_len);
@@ -918,76 +937,86 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
   if (lane < 32) P.part_ml[at] = make_float2(a.m, l);
 }
 
-// The splits of an item's rows joined (blockIdx.x: the item and KV head): D/4 threads take a
-// row's columns, several such teams part many splits and meet in LDS.  A few rows of 64
-// splits are many loads after one another, so an item's rows are spread over gridDim.y.
+// The splits of an item's rows joined: D/4 threads take a row's columns, several such teams
+// part many splits and meet in LDS.  A row of 64 splits, or many rows of 16, are loads after one
+// another, so the rows of an item (and KV head) are up to 32 units of work: as many as there are
+// workgroups for, of the items the host bounds (P.units) where they are few and mostly all
+// split, of those the device counts where they are a last round's.
 template <int D>
 __global__ __launch_bounds__(kThreads) void join_kernel(const Params P) {
   constexpr int kTeam = D / 4, kTeams = kThreads / kTeam;
   __shared__ float4 sums[kTeams][kTeam];
   __shared__ float2 meet[kTeams];   // (max, sum)
-  const int team = threadIdx.x / kTeam, c = threadIdx.x % kTeam, g = blockIdx.x % P.hkv;
-  const int4 rec = P.records[blockIdx.x];
-  if ((int)(blockIdx.x / P.hkv) >= *P.split_items) return;
-  const int splits = rec.x & 0xff, count = rec.w;
-  const int64_t place = (int64_t)(rec.x >> 8) * P.hkv + g;
-  const int teams = splits > 16 ? 8 : splits > 8 ? 4 : splits > 4 ? 2 : 1, rows = kTeams / teams;
-  const int first = team & (teams - 1);
-  for (int row0 = blockIdx.y * rows; row0 < count; row0 += gridDim.y * rows) {
-    const int row = row0 + team / teams;
-    const bool in = row < count;
-    const int64_t at = place * kRows + row, step = (int64_t)P.hkv * kRows;
-    float m = -INFINITY, sum = 0.f;
-    float4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = first; in && s0 < splits; s0 += 4 * teams) {
-      float2 x[4];
-      float4 y[4];
+  const int team = threadIdx.x / kTeam, c = threadIdx.x % kTeam;
+  // records fastest: neighbouring workgroups, on different XCDs, have as many rows to join
+  const int room = P.units ? (int)gridDim.x / P.units : 1;
+  int4 rec = P.records[blockIdx.x % room];   // (not after the count: a latency less)
+  const int records = *P.split_items * P.hkv, stride = P.units ? room : max(records, 1);
+  const int each = P.units ? P.units : max(1, min(kUnits, (int)gridDim.x / stride));
+  for (int unit = blockIdx.x; unit < stride * each; unit += gridDim.x) {
+    const int nth = unit % stride, part = unit / stride;
+    if (nth >= records) return;
+    if (!P.units) rec = P.records[nth];
+    const int splits = rec.x & 0xff, count = rec.w, g = nth % P.hkv;
+    const int64_t place = (int64_t)(rec.x >> 8) * P.hkv + g;
+    const int teams = splits > 16 ? 8 : splits > 8 ? 4 : splits > 4 ? 2 : 1, rows = kTeams / teams;
+    const int first = team & (teams - 1);
+    for (int row0 = part * rows; row0 < count; row0 += each * rows) {
+      const int row = row0 + team / teams;
+      const bool in = row < count;
+      const int64_t at = place * kRows + row, step = (int64_t)P.hkv * kRows;
+      float m = -INFINITY, sum = 0.f;
+      float4 o = {0.f, 0.f, 0.f, 0.f};
+      for (int s0 = first; in && s0 < splits; s0 += 4 * teams) {
+        float2 x[4];
+        float4 y[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {   // the four loads in flight; past the last split: nothing seen
-        const int s = min(s0 + u * teams, splits - 1);
-        x[u] = P.part_ml[at + s * step];
-        y[u] = *(const float4*)(P.part + (at + s * step) * D + c * 4);
-        if (s0 + u * teams >= splits || x[u].y == 0.f) x[u] = make_float2(-INFINITY, 0.f);
-      }
-      const float top = fmaxf(fmaxf(m, fmaxf(x[0].x, x[1].x)), fmaxf(x[2].x, x[3].x));
-      const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-      m = top;
-      sum *= keep;
-      o.x *= keep, o.y *= keep, o.z *= keep, o.w *= keep;
+        for (int u = 0; u < 4; ++u) {   // the four loads in flight; past the last split: nothing seen
+          const int s = min(s0 + u * teams, splits - 1);
+          x[u] = P.part_ml[at + s * step];
+          y[u] = *(const float4*)(P.part + (at + s * step) * D + c * 4);
+          if (s0 + u * teams >= splits || x[u].y == 0.f) x[u] = make_float2(-INFINITY, 0.f);
+        }
+        const float top = fmaxf(fmaxf(m, fmaxf(x[0].x, x[1].x)), fmaxf(x[2].x, x[3].x));
+        const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        m = top;
+        sum *= keep;
+        o.x *= keep, o.y *= keep, o.z *= keep, o.w *= keep;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        if (x[u].y == 0.f) continue;
-        const float f = __builtin_amdgcn_exp2f(x[u].x - m) * x[u].y;
-        sum += f;
-        o.x += f * y[u].x, o.y += f * y[u].y, o.z += f * y[u].z, o.w += f * y[u].w;
+        for (int u = 0; u < 4; ++u) {
+          if (x[u].y == 0.f) continue;
+          const float f = __builtin_amdgcn_exp2f(x[u].x - m) * x[u].y;
+          sum += f;
+          o.x += f * y[u].x, o.y += f * y[u].y, o.z += f * y[u].z, o.w += f * y[u].w;
+        }
       }
-    }
-    if (teams > 1) {
-      __syncthreads();
-      sums[team][c] = o;
-      if (c == 0) meet[team] = make_float2(m, sum);
-      __syncthreads();
-      float top = m;
-      for (int t = 1; t < teams; ++t) top = fmaxf(top, meet[team - first + t].x);
-      const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-      sum *= keep;
-      o.x *= keep, o.y *= keep, o.z *= keep, o.w *= keep;
-      for (int t = 1; t < teams; ++t) {
-        const float2 x = meet[team - first + t];
-        if (x.x == -INFINITY) continue;
-        const float f = __builtin_amdgcn_exp2f(x.x - top);
-        const float4 y = sums[team - first + t][c];
-        sum += f * x.y;
-        o.x += f * y.x, o.y += f * y.y, o.z += f * y.z, o.w += f * y.w;
+      if (teams > 1) {
+        __syncthreads();
+        sums[team][c] = o;
+        if (c == 0) meet[team] = make_float2(m, sum);
+        __syncthreads();
+        float top = m;
+        for (int t = 1; t < teams; ++t) top = fmaxf(top, meet[team - first + t].x);
+        const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        sum *= keep;
+        o.x *= keep, o.y *= keep, o.z *= keep, o.w *= keep;
+        for (int t = 1; t < teams; ++t) {
+          const float2 x = meet[team - first + t];
+          if (x.x == -INFINITY) continue;
+          const float f = __builtin_amdgcn_exp2f(x.x - top);
+          const float4 y = sums[team - first + t][c];
+          sum += f * x.y;
+          o.x += f * y.x, o.y += f * y.y, o.z += f * y.z, o.w += f * y.w;
+        }
       }
-    }
-    if (in && first == 0) {
-      const float f = sum == 0.f ? 0.f : 1.f / sum;
-      const int r = rec.z + row, j = r / P.group, h = r - j * P.group;
-      u32x2 y;
-      y[0] = pack(o.x * f, o.y * f);
-      y[1] = pack(o.z * f, o.w * f);
-      *(u32x2*)(P.out + ((int64_t)(rec.y + j) * P.hq + g * P.group + h) * D + c * 4) = y;
+      if (in && first == 0) {
+        const float f = sum == 0.f ? 0.f : 1.f / sum;
+        const int r = rec.z + row, j = r / P.group, h = r - j * P.group;
+        u32x2 y;
+        y[0] = pack(o.x * f, o.y * f);
+        y[1] = pack(o.z * f, o.w * f);
+        *(u32x2*)(P.out + ((int64_t)(rec.y + j) * P.hq + g * P.group + h) * D + c * 4) = y;
+      }
     }
   }
 }
@@ -1143,8 +1172,10 @@ extern "C" nsd_status nsd_chunk_attention(
   if (const nsd_status st = check_launch(fn)) return st;
   if (pl.places) {
     // about four workgroups a CU
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(32, 1024 / split_items));
-    const dim3 grid((uint32_t)split_items, (uint32_t)parts);
+    P.units = pl.items * num_kv_heads > kSlots
+                  ? 0 : (int)std::max<int64_t>(1, std::min<int64_t>(kUnits, 2 * kSlots / split_items));
+    const dim3 grid((uint32_t)(P.units ? split_items * P.units
+                                       : std::min<int64_t>(split_items * kUnits, 2 * kSlots)));
     if (head_dim == 64)
       hipLaunchKernelGGL(join_kernel<64>, grid, dim3(kThreads), 0, (hipStream_t)stream, P);
     else

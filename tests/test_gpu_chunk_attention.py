@@ -185,6 +185,14 @@ def test_batches_placed_by_length(device, bs, hkv, ctx_hi):
     Batch(device, ctx.tolist(), new.tolist(), 2 * hkv, hkv, 64, seed=bs).check()
 
 
+@pytest.mark.parametrize("ctx, new", [([600], [272]), ([300, 500], [200, 90])])
+def test_a_last_round_of_few_items(device, ctx, new):
+    """17 to 19 items where 16 run at once: those of the last round are split."""
+    b = Batch(device, ctx, new, 256, 32, 64)
+    pos = np.concatenate([np.arange(c, c + n) for c, n in zip(b.ctx, b.new)])
+    b.check(first=np.maximum(pos - 400, 0), prefix=[30] * len(ctx))
+
+
 def test_rows_behind_the_last_request_stay(device):
     b = Batch(device, [30, 500, 2], [20, 1, 7], 4, 2, 64)
     dev, pad = device, 300
