@@ -35,6 +35,7 @@
 // 4096 tokens 530 us, 1038 TFLOP/s; 256 single tokens at 1-4k 416 us, 6.5 TB/s; 128 of them at
 // 2-8k, capped, in a window of 1024 behind a prefix 100 us, 5.7 TB/s.  128 rows rather than 256:
 // two workgroups of four waves on a CU rather than one of eight, which all wait at one barrier.
+#include "chunk_plan.h"
 #include "nsd_internal.h"
 
 #include <algorithm>
@@ -51,19 +52,10 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
 
-constexpr int kMaxBatch = 8192;
-constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
-constexpr int kWaveRows = 32;
-constexpr int kRows = kWaves * kWaveRows;    // query rows (token, head of the group) of an item, at most
-constexpr int kStage = 64;                   // tokens of a stage
 constexpr int kStageBlocks = kStage / NSD_BLOCK_SIZE;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kSlack = 8.f;                // log2 of the weights' bound
-constexpr int kSlots = 512;                  // workgroups resident on 256 CUs, two each
-constexpr int kPerLane = 4;                  // requests a lane looks at where the batch is parted
-constexpr int kPartedBatch = 64 * kPerLane;
-constexpr int kMaxSplits = 64;
 constexpr int kUnits = 32;                   // of an item's rows, at most, in the join
 
 struct Params {
@@ -155,18 +147,20 @@ struct Piece {
 // The idx-th piece of a batch of at most kPartedBatch requests, found by every wave from the
 // batch's lengths (a lane has up to four requests), so that no launch and no list goes before.
 //
-// A tile's cost is the stages its request's tokens span.  A slot's fair share of the batch is
-// total / (kSlots / hkv).  Where the tiles are fewer than the slots, they are split so that all
-// pieces run in one round; where they are more, only a tile of more than 1.5 shares is (a part
-// costs its rows' partial results, written and read), or, if there is none, those that would
-// begin a last round less than half full.  Long pieces go first, in five classes of length.
-// All waves compute the same from the same lengths.
+// A tile's cost is the stages its request's tokens span (split_limit() and last_round() say
+// which are split).  Long pieces go first, in five classes of length.  All waves compute the same
+// from the same lengths.
+//
+// Offsets that fall (no valid batch's) count tokens twice, and the items may pass the host's
+// bound: such a batch is not split, so that no part or record lacks its workgroup, and items past
+// the grid are left out.
 __device__ inline Piece find_piece(const Params& P, const int32_t* indptr, const int32_t* lens,
                                    const int32_t* prefixes, int idx) {
   const int lane = threadIdx.x & 63, per = (P.bs + 63) / 64;
   int tiles[kPerLane], stages[kPerLane], splits[kPerLane], base[kPerLane], nth[kPerLane];
   float cost = 0.f;
   int count = 0;
+  bool falls = false;
   int a[kPerLane], b[kPerLane], L[kPerLane], prefix[kPerLane], first[kPerLane];
 #pragma unroll
   for (int i = 0; i < kPerLane; ++i) {   // (all the loads in flight)
@@ -179,7 +173,9 @@ __device__ inline Piece find_piece(const Params& P, const int32_t* indptr, const
 #pragma unroll
   for (int i = 0; i < kPerLane; ++i) {
     a[i] = min(max(a[i], 0), P.total_q);
-    b[i] = min(max(b[i], a[i]), P.total_q);
+    b[i] = min(max(b[i], 0), P.total_q);
+    falls |= b[i] < a[i];
+    b[i] = max(b[i], a[i]);
     first[i] = P.first ? P.first[min(a[i], P.total_q - 1)] : 0;
   }
 #pragma unroll
@@ -198,15 +194,15 @@ __device__ inline Piece find_piece(const Params& P, const int32_t* indptr, const
   const auto larger = [](float x, float y) { return fmaxf(x, y); };
   const float total = last_lane(wave_scan(cost, 0.f, add));
   const int items = last_lane(sum_scan(count));
-  int tail = 0, tail_splits = 1;
+  Tail tail{0, 1};
   if (P.max_places) {
-    const float slots = (float)kSlots / P.hkv;
-    const float limit = fmaxf(items < slots ? total / (slots - 0.5f * items) : 1.5f * total / slots, 4.f);
+    const bool rising = !__ballot(falls);
+    const float limit = rising ? split_limit(items, total, P.hkv) : INFINITY;
     int places = 0, split_items = 0;
 #pragma unroll
     for (int i = 0; i < kPerLane; ++i) {
       if (i >= per) continue;
-      splits[i] = min((int)ceilf(stages[i] / limit), kMaxSplits);
+      splits[i] = parts_of(stages[i], limit);
       const int y = splits[i] > 1 ? tiles[i] : 0, x = y * splits[i];
       const int upto = sum_scan(x), nth_upto = sum_scan(y);
       base[i] = places + upto - x;
@@ -219,22 +215,19 @@ __device__ inline Piece find_piece(const Params& P, const int32_t* indptr, const
       for (int i = 0; i < kPerLane; ++i) splits[i] = 1;
       split_items = 0;
     }
-    const int round = kSlots / P.hkv, over = round ? items % round : 0;
-    if (split_items == 0 && items > round && over > 0 && 2 * over <= round) {
-      // two ragged chunks (194 tiles a head) 2897 -> 2530 us, 8300 tokens after 24000 3712 -> 3400
-      tail = over;
-      tail_splits = min(round / over, 16);
-      split_items = tail;
+    if (rising && split_items == 0) {
+      tail = last_round(items, P.hkv);
+      split_items = tail.items;
     }
     if (blockIdx.x == 0 && threadIdx.x == 0) *P.split_items = split_items;
   }
   int mine = 0;
 #pragma unroll
   for (int i = 0; i < kPerLane; ++i) mine += tiles[i] * splits[i];
-  const int whole = last_lane(sum_scan(mine)) - tail, pieces = whole + tail * tail_splits;
+  const int whole = last_lane(sum_scan(mine)) - tail.items, pieces = whole + tail.items * tail.parts;
   if (idx >= pieces) return Piece{-1};
-  const int part = idx < whole ? 0 : (idx - whole) % tail_splits;
-  const int nth_tail = idx < whole ? -1 : (idx - whole) / tail_splits;
+  const int part = idx < whole ? 0 : (idx - whole) % tail.parts;
+  const int nth_tail = idx < whole ? -1 : (idx - whole) / tail.parts;
   if (nth_tail >= 0) idx = whole + nth_tail;
   float most = 0.f, each[kPerLane];
 #pragma unroll
@@ -266,9 +259,9 @@ __device__ inline Piece find_piece(const Params& P, const int32_t* indptr, const
         p.place = n > 1 ? at(base[i]) + p.tile * n + p.split : 0;
         p.record = n > 1 ? at(nth[i]) + p.tile : 0;
         if (nth_tail >= 0) {   // (no request is split besides)
-          p.splits = tail_splits;
+          p.splits = tail.parts;
           p.split = part;
-          p.place = nth_tail * tail_splits + part;
+          p.place = nth_tail * tail.parts + part;
           p.record = nth_tail;
         }
         p.a0 = at(a[i]);
@@ -1021,51 +1014,11 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Params P) {
   }
 }
 
-// Bounds per KV head: a batch's items, the split ones of them and their parts.
-struct Plan {
-  int tile;        // rows of an item
-  int64_t items;
-  int split_items, places;
-};
-
-Plan plan(int32_t bs, int32_t total_q, int32_t hq, int32_t hkv, int32_t max_len) {
-  Plan p;
-  const int64_t stages = ((int64_t)max_len + kStage - 1) / kStage;
-  // Where items of 32 or 64 rows still run all at once, their waves part the tokens of short
-  // contexts: up to 2048 tokens that is faster than 128 rows after one another (512 tokens of a
-  // new request 15.5 -> 13.1 us, four of 350-900 at head_dim 64 20.1 -> 13.6), beyond it the
-  // planes are read too often (512 after 8000 88 -> 131 us).
-  p.tile = kRows;
-  while (stages <= 32 && p.tile > kWaveRows &&
-         ((int64_t)total_q * (hq / hkv) / (p.tile / 2) + bs) * hkv <= kSlots)
-    p.tile /= 2;
-  p.items = (int64_t)total_q * (hq / hkv) / p.tile + bs;
-  // The second launch does not pay for itself where the items make two rounds or more of
-  // contexts to 8192 tokens (packed documents, 4 requests to 6000 tokens: 105 us without, 122
-  // with it), nor where all are short; one much longer item among many does.
-  p.split_items = p.places = 0;
-  if (bs > kPartedBatch || stages <= (p.items * hkv > 2 * kSlots ? 129 : 12)) return p;
-  // A tile of s stages has at most 1 + s / limit <= 2 s / limit parts if it is split, and the
-  // tiles' s sum to the total: at most 2 total / limit places, where limit is at least the
-  // share total / (kSlots / hkv); also at most kMaxSplits and ceil(stages / 4) a tile.
-  const int64_t share = 2 * kSlots / hkv + 1;
-  const int64_t each = std::min<int64_t>(kMaxSplits, (stages + 3) / 4);
-  p.places = (int)std::min(share, p.items * each);
-  p.split_items = (int)std::min<int64_t>(p.places / 2, p.items);
-  return p;
-}
-
 bool sizes_ok(int32_t bs, int32_t total_q, int32_t hq, int32_t hkv, int32_t d, int32_t max_q,
               int32_t max_len) {
   return bs >= 0 && bs <= kMaxBatch && total_q >= 0 && hkv >= 1 && hq >= hkv && hq % hkv == 0 &&
          (d == 64 || d == 128) && max_q >= 1 && max_len >= 1 &&
          (int64_t)total_q * hq <= INT32_MAX;
-}
-
-size_t workspace_bytes(const Plan& p, int32_t hkv, int32_t d) {
-  // the count, the records, then (max, sum) and rows of every place
-  return p.places ? 16 + (size_t)p.split_items * hkv * 16 +
-                        (size_t)p.places * hkv * kRows * (8 + (size_t)d * 4) : 0;
 }
 
 }  // namespace
@@ -1120,9 +1073,7 @@ extern "C" nsd_status nsd_chunk_attention(
   if (need && (!workspace || workspace_size < need || (uintptr_t)workspace % 16))
     return fail(NSD_ERR_WORKSPACE, "%s: a 16-byte aligned workspace of %zu bytes needed, %zu given",
                 fn, need, workspace ? workspace_size : (size_t)0);
-  // parts beyond the first of each item: fewer than total / limit
-  const int64_t parts = std::min(pl.places, kSlots / num_kv_heads + 1);
-  const int64_t groups = (pl.items + parts) * num_kv_heads;
+  const int64_t groups = pieces(pl, num_kv_heads) * num_kv_heads;
   if (groups > INT32_MAX) return fail(NSD_ERR_UNSUPPORTED, "%s: too many workgroups", fn);
   Params P;
   P.q = (const uint16_t*)q;

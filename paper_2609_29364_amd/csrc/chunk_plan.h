@@ -1,0 +1,98 @@
+// How a batch of chunk_attention becomes items (at most 128 rows of a KV head) and parts of them:
+// the host's bounds, which size the grid and the workspace, and the device's rules, by which every
+// wave finds its piece from the batch's lengths (no device types, so that the counts can be checked
+// by themselves).
+#pragma once
+
+#include <algorithm>
+#include <cstddef>
+#include <cstdint>
+
+namespace {
+
+constexpr int kMaxBatch = 8192;
+constexpr int kWaves = 4;
+constexpr int kWaveRows = 32;
+constexpr int kRows = kWaves * kWaveRows;    // query rows (token, head of the group) of an item, at most
+constexpr int kStage = 64;                   // tokens of a stage
+constexpr int kSlots = 512;                  // workgroups resident on 256 CUs, two each
+constexpr int kPerLane = 4;                  // requests a lane looks at where the batch is parted
+constexpr int kPartedBatch = 64 * kPerLane;
+constexpr int kMaxSplits = 64;
+
+// The most stages a part has.  A slot's fair share of the batch is total / (kSlots / hkv) stages.
+// Where the items are fewer than the slots, they are split so that all pieces run in one round
+// (the parts beyond the first of each are fewer than total / limit); where they are more, only
+// one of more than 1.5 shares is: a part costs its rows' partial results, written and read.
+constexpr float split_limit(int items, float total, int hkv) {
+  const float slots = (float)kSlots / hkv;
+  const float limit = items < slots ? total / (slots - 0.5f * items) : 1.5f * total / slots;
+  return limit > 4.f ? limit : 4.f;
+}
+
+// Parts of an item of `stages` stages.
+constexpr int parts_of(int stages, float limit) {
+  const float x = stages / limit;
+  const int n = (int)x;
+  return std::max(1, std::min(n + (n < x), kMaxSplits));
+}
+
+// Where none is split so, the items that would begin a last round less than half full are split
+// to fill it: two ragged chunks (194 tiles a head) 2897 -> 2530 us, 8300 tokens after 24000 3712
+// -> 3400.
+struct Tail {
+  int items, parts;
+};
+constexpr Tail last_round(int items, int hkv) {
+  const int round = kSlots / hkv, over = round ? items % round : 0;
+  if (items <= round || over == 0 || 2 * over > round) return Tail{0, 1};
+  return Tail{over, std::min(round / over, 16)};
+}
+
+// Bounds per KV head: a batch's items, the split ones of them and their parts.
+struct Plan {
+  int tile;        // rows of an item
+  int64_t items;
+  int split_items, places;
+};
+
+Plan plan(int32_t bs, int32_t total_q, int32_t hq, int32_t hkv, int32_t max_len) {
+  Plan p;
+  const int64_t stages = ((int64_t)max_len + kStage - 1) / kStage;
+  // Where items of 32 or 64 rows still run all at once, their waves part the tokens of short
+  // contexts: up to 2048 tokens that is faster than 128 rows after one another (512 tokens of a
+  // new request 15.5 -> 13.1 us, four of 350-900 at head_dim 64 20.1 -> 13.6), beyond it the
+  // planes are read too often (512 after 8000 88 -> 131 us).
+  p.tile = kRows;
+  while (stages <= 32 && p.tile > kWaveRows &&
+         ((int64_t)total_q * (hq / hkv) / (p.tile / 2) + bs) * hkv <= kSlots)
+    p.tile /= 2;
+  p.items = (int64_t)total_q * (hq / hkv) / p.tile + bs;
+  // The second launch does not pay for itself where the items make two rounds or more of
+  // contexts to 8192 tokens (packed documents, 4 requests to 6000 tokens: 105 us without, 122
+  // with it), nor where all are short; one much longer item among many does.
+  p.split_items = p.places = 0;
+  if (bs > kPartedBatch || stages <= (p.items * hkv > 2 * kSlots ? 129 : 12)) return p;
+  // A tile of s stages has at most 1 + s / limit <= 2 s / limit parts if it is split, and the
+  // tiles' s sum to the total: at most 2 total / limit places, where limit is at least the
+  // share total / (kSlots / hkv); also at most kMaxSplits and ceil(stages / 4) a tile.
+  const int64_t share = 2 * kSlots / hkv + 1;
+  const int64_t each = std::min<int64_t>(kMaxSplits, (stages + 3) / 4);
+  p.places = (int)std::min(share, p.items * each);
+  p.split_items = (int)std::min<int64_t>(p.places / 2, p.items);
+  return p;
+}
+
+size_t workspace_bytes(const Plan& p, int32_t hkv, int32_t d) {
+  // the count, the records, then (max, sum) and rows of every place
+  return p.places ? 16 + (size_t)p.split_items * hkv * 16 +
+                        (size_t)p.places * hkv * kRows * (8 + (size_t)d * 4) : 0;
+}
+
+// Workgroups per KV head: the items, and parts beyond the first of each, which are fewer than
+// total / limit.
+int64_t pieces(const Plan& p, int32_t hkv) {
+  return p.items + std::min(p.places, kSlots / hkv + 1);
+}
+
+}  // namespace
