@@ -634,8 +634,8 @@ nsd_status nsd_rope_append(void* k_pool, void* v_pool, int64_t num_blocks, const
  *     request sees, also those after it (clamped to [0, L_r]).
  * slopes : device fp32 [num_q_heads], finite, or NULL.  softcap >= 0, finite.
  * seq_lens : L_r beyond max_seq_len or the table's row are clamped.  A request
- *     may have no new token; one with L_r < n_q has rows that see nothing
- *     before position 0.
+ *     may have no new token; in one with L_r < n_q the rows before position 0
+ *     see their request's prefix and nothing else.
  * total_q : rows of q and out; q_indptr entries are clamped into [0, total_q].
  *     total_q * num_q_heads <= 2^31 - 1.  max_q_per_seq >= 1 bounds n_q.
  * head_dim in {64, 128}; any num_q_heads / num_kv_heads; block_size == 16;

@@ -646,6 +646,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
   const int count = (int)min(rows - row0, (int64_t)P.tile);
   const int rgroups = count <= kWaveRows ? 1 : count <= 2 * kWaveRows ? 2 : kWaves;
   const int rg = wave & (rgroups - 1), tgroups = kWaves / rgroups, tg = wave / rgroups;
+  const bool idle = rg * kWaveRows >= count;   // a wave without rows
 
   // this lane's row
   const int64_t row = row0 + rg * kWaveRows + (lane & 31);
@@ -684,8 +685,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
   }
   const int64_t wave_last = min(row0 + count, row0 + (rg + 1) * kWaveRows) - 1;
   const int pmin = min(L - n + (int)((row0 + rg * kWaveRows) / P.group), last);
-  const int pmax = wave_last >= row0 + rg * kWaveRows
-                       ? min(L - n + (int)(wave_last / P.group), last) : -1;
+  const int pmax = min(L - n + (int)(wave_last / P.group), last);
   const int low = min(L - n + (int)(row0 / P.group), last);   // the workgroup's first position
   const int to = min(L - n + (int)((row0 + count - 1) / P.group), last) + 1;   // past its last key
   // stages: those of the prefix, then from the first key's on
@@ -757,7 +757,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
   };
   auto seen_by_some = [&](int i, uint32_t valid, const uint16_t* buf) {
     const int t0 = start(i);
-    if (pmax < 0) return;
+    if (idle) return;
     for (int u = 0; u < 2; ++u) {
       const int t = t0 + u * 32;
       const uint32_t ok = valid >> (2 * u) & 3;
@@ -875,7 +875,7 @@ __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
     for (int i = i0; i < i1; i += 2) {
       while (i + 1 < i1) {   // the hot loop
         vb = seek(start(i + 1));
-        if (!(open(i, va) & open(i + 1, vb)) | (pmax < 0)) break;
+        if (!(open(i, va) & open(i + 1, vb)) | idle) break;
         arrived();
         load(start(i + 1), vb, buf1);
         seen_by_all(i, buf0);

@@ -1,9 +1,12 @@
-"""Chunk attention at the edges of what its call allows."""
+"""Chunk attention at the edges of what its call allows, against the oracle under the bounds of
+test_gpu_chunk_attention.py."""
+import numpy as np
 import pytest
 import torch
 
 import paper_2609_29364_amd as nsd
 from parity import i32
+from test_gpu_chunk_attention import Batch, both_sizes
 
 pytestmark = pytest.mark.gpu
 
@@ -31,3 +34,22 @@ def test_offsets_that_fall_stay_in_bounds(device, indptr, length, hq, hkv, d, ma
         assert (room[:256] == fill).all() and (room[256 + need:] == fill).all()
         # averages of V, or untouched
         assert torch.isfinite(out).all() and out.abs().max() <= 7
+
+
+@both_sizes
+@pytest.mark.parametrize("slopes", [None, [0.0, 0.05, 0.003, 0.2]])
+def test_rows_before_position_0_see_the_prefix(device, slopes, bound):
+    """Requests shorter than their new tokens: whole waves of rows before position 0, and waves
+    that hold rows of both kinds."""
+    b = Batch(device, [0, 0, 0], [300, 90, 70], 4, 2, 64)
+    b.lens = [40, 20, 64]
+    b.kv = [[x[:n] for x in kv] for kv, n in zip(b.kv, b.lens)]
+    prefix = [33, 70, 0]
+    kw = dict(prefix=prefix) if slopes is None else dict(prefix=prefix, slopes=slopes)
+    got = b.run(bound=bound, **kw).double().cpu().numpy()
+    ref, tol = b.ref(**kw)
+    # distances reach 300, past the lengths that the bound takes
+    tol = tol + 2.0**-21 * (0.2 * 300 if slopes else 0) * 5
+    assert (np.abs(got - ref) <= tol).all()
+    assert (np.abs(got[:260]).max((1, 2)) > 0).all()      # the prefix alone
+    assert (got[390:396] == 0).all()                      # no prefix: nothing
