@@ -57,6 +57,9 @@ constexpr int kStageBlocks = kStage / NSD_BLOCK_SIZE;
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kSlack = 8.f;                // log2 of the weights' bound
 constexpr int kUnits = 32;                   // of an item's rows, at most, in the join
+// CAP of the templates below: scores are not capped, capped at up to kUsual, or at more.
+enum { kNoCap, kUsualCap, kLargeCap };
+constexpr float kUsual = 256.f;
 
 struct Params {
   const uint16_t* q;
@@ -304,7 +307,7 @@ struct Sight {
   static __device__ inline uint32_t below(int n) { return (1u << min(max(n, 0), 8)) - 1; }
 };
 
-// MFMA operands from a block's tiles.  CAP: capped scores; BIAS: slopes.
+// MFMA operands from a block's tiles.
 template <int D>
 struct Tile {
   static constexpr int kHalf = D * 16;   // elements of a block's K or V tile
@@ -379,20 +382,34 @@ __device__ inline bf16x8 ones(uint32_t m) {
 }
 
 // Scores of NSUB x 32 tokens from t0 on, capped and biased, to the log2 domain (c: scale log2 e).
-template <bool CAP, bool BIAS, int NSUB>
+//
+// The cap as 1 - 2 / (1 + e^(2 x / cap)) takes two numbers of its own size from one another: off by
+// 2^-22 of the cap or so whatever the score, which up to kUsual is 2^-14 of a weight, a 64th of
+// its rounding to bf16.  kLargeCap, for caps beyond: the series of tanh where |x / cap| < 1/4 (its
+// next term is 2^-26 of the score there), so that the error is about 5 2^-23 of the score itself.
+template <int CAP, bool BIAS, int NSUB>
 __device__ inline void to_log2(f32x16 (&s)[NSUB], float c, float cap, const Sight& w, int t0,
                                int half) {
-  const float y = CAP ? fminf(2.f * c / cap, 3e38f) : 0.f, top = cap * kLog2e;
+  const float y = CAP ? fminf(2.f * c / cap, 3e38f) : 0.f;
+  const float top = fminf(cap * kLog2e, 3e38f), u1 = c / top;
   const float d0 = (float)(w.p - t0 - 8 * half);
 #pragma unroll
   for (int u = 0; u < NSUB; ++u)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       float x;
-      if constexpr (CAP) {
+      if constexpr (CAP == kUsualCap) {
         // cap tanh(x / cap): 1 - 2 / (1 + e^(2 x / cap))
         const float e = __builtin_amdgcn_exp2f(s[u][i] * y);
         x = fmaf(-2.f * top, __builtin_amdgcn_rcpf(1.f + e), top);
+      } else if constexpr (CAP == kLargeCap) {
+        const float v = s[u][i] * u1, vv = v * v;
+        const float e = __builtin_amdgcn_exp2f(s[u][i] * y);
+        const float far = top * fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + e), 1.f);
+        const float series =
+            vv * fmaf(vv, fmaf(vv, fmaf(vv, 62.f / 2835, -17.f / 315), 2.f / 15), -1.f / 3);
+        x = s[u][i] * c;
+        x = fabsf(v) < 0.25f ? fmaf(x, series, x) : far;
       } else {
         x = s[u][i] * c;
       }
@@ -420,7 +437,7 @@ __device__ inline void grow(Acc<D>& a, float top) {
 // Softmax and the second product of NSUB x 32 tokens from t0 on for a wave's rows: s their
 // S^T, values(b, t) the V^T operand of block b's dimensions 32 t...  hidden: some row may not
 // see some token.  valid: bit b set if block b may be read.
-template <int D, bool CAP, bool BIAS, int NSUB, class Values>
+template <int D, int CAP, bool BIAS, int NSUB, class Values>
 __device__ inline void weigh(Acc<D>& a, f32x16 (&s)[NSUB], const Values& values, const Params& P,
                              const Sight& w, int t0, uint32_t valid, bool hidden) {
   const int half = (threadIdx.x & 63) >> 5;
@@ -513,7 +530,7 @@ __device__ inline void add_infinities(Acc<D>& a, const uint16_t* v, const Sight&
 }
 
 // weigh() from a stage's tiles in LDS.
-template <int D, bool CAP, bool BIAS, int NSUB>
+template <int D, int CAP, bool BIAS, int NSUB>
 __device__ inline void stage(Acc<D>& a, const uint16_t* k, const uint16_t* v,
                              const bf16x8 (&q)[D / 16], const Params& P, const Sight& w, int t0,
                              uint32_t valid, bool hidden) {
@@ -608,7 +625,7 @@ __device__ inline void open_stage(Acc<D>& a, const uint16_t* k, const uint16_t* 
   __builtin_amdgcn_sched_group_barrier(0x008, VT, 1);
 }
 
-template <int D, bool CAP, bool BIAS>
+template <int D, int CAP, bool BIAS>
 __global__ __launch_bounds__(kThreads, 2) void chunk_kernel(
     const Params P, const int32_t* __restrict__ tables, const int32_t* __restrict__ lens,
     const int32_t* __restrict__ indptr, const int32_t* __restrict__ prefixes) {
@@ -1112,14 +1129,17 @@ extern "C" nsd_status nsd_chunk_attention(
     hipLaunchKernelGGL(kernel, dim3((uint32_t)groups), dim3(kThreads), 0, (hipStream_t)stream, P,
                        block_table, seq_lens, q_indptr, prefix_lens);
   };
-  const bool cap = softcap > 0.f, bias = slopes != nullptr;
-  if (head_dim == 64) {
-    if (cap) bias ? go(chunk_kernel<64, true, true>) : go(chunk_kernel<64, true, false>);
-    else bias ? go(chunk_kernel<64, false, true>) : go(chunk_kernel<64, false, false>);
-  } else {
-    if (cap) bias ? go(chunk_kernel<128, true, true>) : go(chunk_kernel<128, true, false>);
-    else bias ? go(chunk_kernel<128, false, true>) : go(chunk_kernel<128, false, false>);
-  }
+  const bool bias = slopes != nullptr;
+  auto capped = [&](auto d, auto biased) {
+    constexpr int D = decltype(d)::value;
+    constexpr bool kBias = decltype(biased)::value;
+    if (softcap == 0.f) go(chunk_kernel<D, kNoCap, kBias>);
+    else if (softcap <= kUsual) go(chunk_kernel<D, kUsualCap, kBias>);
+    else go(chunk_kernel<D, kLargeCap, kBias>);
+  };
+  auto dims = [&](auto d) { bias ? capped(d, std::true_type{}) : capped(d, std::false_type{}); };
+  if (head_dim == 64) dims(std::integral_constant<int, 64>{});
+  else dims(std::integral_constant<int, 128>{});
   if (const nsd_status st = check_launch(fn)) return st;
   if (pl.places) {
     // about four workgroups a CU

@@ -53,3 +53,32 @@ def test_rows_before_position_0_see_the_prefix(device, slopes, bound):
     assert (np.abs(got - ref) <= tol).all()
     assert (np.abs(got[:260]).max((1, 2)) > 0).all()      # the prefix alone
     assert (got[390:396] == 0).all()                      # no prefix: nothing
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("slopes", [None, [0.25, 1.0, 0.0, -0.01]])
+@pytest.mark.parametrize("softcap, scale", [(200.0, None), (256.0, None), (257.0, None), (1e3, None),
+                                            (3e4, -0.2), (1e6, None), (1e8, None), (3e38, None),
+                                            (300.0, 8.0), (1e4, 300.0), (1e4, -1000.0)])
+def test_large_caps(device, softcap, scale, slopes, d):
+    """A cap far above the scores leaves them alone, one among large scores bends them.
+
+    A capped score is off by a few 2^-23 of itself where it is formed, and from the product by what
+    the scale makes of 128 * 2^-24 * sum |q k|: both in a weight and in the maximum."""
+    b = Batch(device, [0, 130, 300], [70, 1, 40], 4, 2, d)
+    ref, tol = b.ref(scale=scale, softcap=softcap, slopes=slopes)
+    v = np.abs(np.concatenate([x[1].float().numpy().reshape(-1) for x in b.kv])).max()
+    top = min(softcap, abs(scale or d ** -0.5) * 6 * d)
+    product = abs(scale or d ** -0.5) * 128 * 2.0**-24 * 2 * d
+    tol = tol + 2 * (8 * 2.0**-23 * top + product) * v
+    for bound in (0, 5000):
+        got = b.run(scale=scale, softcap=softcap, slopes=slopes, bound=bound).double().cpu().numpy()
+        assert (np.abs(got - ref) <= tol).all()
+
+
+@pytest.mark.parametrize("bs", [300, 256])
+def test_capped_single_tokens_of_many_requests(device, bs):
+    rng = np.random.default_rng(bs)
+    b = Batch(device, rng.integers(0, 200, bs).tolist(), [1] * bs, 4, 2, 64)
+    b.check(softcap=5.0)
+    b.check(softcap=1e5)
