@@ -1012,7 +1012,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const Params P) {
         o.x *= keep, o.y *= keep, o.z *= keep, o.w *= keep;
         for (int t = 1; t < teams; ++t) {
           const float2 x = meet[team - first + t];
-          if (x.x == -INFINITY) continue;
+          if (x.y == 0.f) continue;   // (the sum of NaN scores is NaN, their maximum -infinity)
           const float f = __builtin_amdgcn_exp2f(x.x - top);
           const float4 y = sums[team - first + t][c];
           sum += f * x.y;

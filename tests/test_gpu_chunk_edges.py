@@ -82,3 +82,14 @@ def test_capped_single_tokens_of_many_requests(device, bs):
     b = Batch(device, rng.integers(0, 200, bs).tolist(), [1] * bs, 4, 2, 64)
     b.check(softcap=5.0)
     b.check(softcap=1e5)
+
+
+@pytest.mark.parametrize("length, every, nth", [(1500, 2, 1), (4096, 4, 1), (4096, 4, 3), (4096, 1, 0),
+                                                (4096, 16, 7)])
+def test_parts_of_nan_scores_reach_the_row(device, length, every, nth):
+    """A split context of which every so many parts (256 tokens each) have no score but NaN."""
+    b = Batch(device, [length - 1], [1], 4, 2, 64)
+    for t in range(length):
+        if t // 256 % every == nth:
+            b.put(0, t, k=float("nan"))
+    assert torch.isnan(b.run(bound=length)).all()
