@@ -1111,8 +1111,9 @@ extern "C" nsd_status nsd_chunk_attention(
   P.parted = pl.places || (max_seq_len > 12 * kStage && bs >= 16 && bs <= kPartedBatch && pl.items * num_kv_heads > kSlots &&
                            pl.items * num_kv_heads <= 8 * kSlots);
   P.num_blocks = num_blocks;
-  // 0 becomes a factor too small to move a weight, as 0 times a hidden token's -infinity is NaN
-  P.scale = std::max(std::fabs(scale) * kLog2e, 1e-37f);
+  // 0 becomes a factor too small to move a weight, as 0 times a hidden token's -infinity is NaN;
+  // nor is it infinite, as that times a score of 0 is too
+  P.scale = std::min(std::max(std::fabs(scale) * kLog2e, 1e-37f), 3e38f);
   P.cap = softcap;
   P.negate = std::signbit(scale) ? 0x80008000u : 0u;
   P.width = max_blocks_per_seq;

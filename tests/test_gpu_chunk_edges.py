@@ -93,3 +93,14 @@ def test_parts_of_nan_scores_reach_the_row(device, length, every, nth):
         if t // 256 % every == nth:
             b.put(0, t, k=float("nan"))
     assert torch.isnan(b.run(bound=length)).all()
+
+
+@both_sizes
+@pytest.mark.parametrize("softcap", [0.0, 20.0])
+@pytest.mark.parametrize("scale", [3e38, -3e38])
+def test_the_largest_scale(device, scale, softcap, bound):
+    b = Batch(device, [40], [50], 2, 1, 64)
+    b.q.zero_()
+    got = b.run(scale=scale, softcap=softcap, bound=bound).double().cpu().numpy()
+    ref, tol = b.ref(scale=0.0)                           # every score is 0
+    assert (np.abs(got - ref) <= tol).all()
