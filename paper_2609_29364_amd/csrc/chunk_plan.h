@@ -80,6 +80,7 @@ Plan plan(int32_t bs, int32_t total_q, int32_t hq, int32_t hkv, int32_t max_len)
   const int64_t each = std::min<int64_t>(kMaxSplits, (stages + 3) / 4);
   p.places = (int)std::min(share, p.items * each);
   p.split_items = (int)std::min<int64_t>(p.places / 2, p.items);
+  if (p.split_items == 0) p.places = 0;   // (more KV heads than workgroups to split for)
   return p;
 }
 

@@ -130,3 +130,13 @@ def test_any_contents(count):
         else:
             unsound += not sound(count(indptr, lens, total, hq, hkv, max_len, trusting=1))
     assert split > 300 and last > 30 and unsound > 10     # the batches reach all of it
+
+
+@pytest.mark.parametrize("hkv", [1, 8, 512, 513, 1024, 1025, 2048, 65536])
+@pytest.mark.parametrize("max_len", [1, 769, 8257, 32768, 2**31 - 1])
+def test_room_for_parts_has_room_for_their_records(count, hkv, max_len):
+    """The join's grid is of records: with places and no record it would be one of nothing."""
+    for bs, total in ((1, 1), (2, 300), (256, 256), (257, 257), (8192, 8192)):
+        c = count([0] * bs + [total], [max_len] * bs, total, hkv, hkv, max_len)
+        assert (c["room"] == 0) == (c["records"] == 0), (bs, total)
+        assert c["records"] * 2 <= c["room"] and sound(c)

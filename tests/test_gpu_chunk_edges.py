@@ -104,3 +104,10 @@ def test_the_largest_scale(device, scale, softcap, bound):
     got = b.run(scale=scale, softcap=softcap, bound=bound).double().cpu().numpy()
     ref, tol = b.ref(scale=0.0)                           # every score is 0
     assert (np.abs(got - ref) <= tol).all()
+
+
+@pytest.mark.parametrize("hkv", [513, 1024, 1025, 2050])
+def test_more_heads_than_workgroups_at_once(device, hkv):
+    b = Batch(device, [40, 0], [1, 18], hkv, hkv, 64)
+    b.check()
+    b.check(b.run(bound=10000))
