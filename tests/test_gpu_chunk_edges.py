@@ -111,3 +111,18 @@ def test_more_heads_than_workgroups_at_once(device, hkv):
     b = Batch(device, [40, 0], [1, 18], hkv, hkv, 64)
     b.check()
     b.check(b.run(bound=10000))
+
+
+def test_one_long_context_among_many_items(device):
+    """More (item, KV head) pairs than two rounds take, with one context far longer than the rest,
+    past the lengths up to which such batches are not split."""
+    bs = 140
+    rng = np.random.default_rng(1)
+    ctx, new = rng.integers(0, 60, bs), np.ones(bs, int)
+    ctx[77], new[3] = 9000, 90
+    b = Batch(device, ctx.tolist(), new.tolist(), 16, 8, 64)
+    assert nsd.chunk_attention_workspace_size(bs, b.total, 16, 8, 64, 90, max(b.lens)) > 0
+    b.check(b.run())
+    pos = np.concatenate([np.arange(c, c + n) for c, n in zip(b.ctx, b.new)])
+    kw = dict(first=np.maximum(pos - 8000, 0), prefix=[20] * bs, softcap=30.0)
+    b.check(b.run(**kw), **kw)
