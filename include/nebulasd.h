@@ -536,7 +536,9 @@ nsd_status nsd_sample_steps(const float* probs, int64_t row_stride, const float*
  * slot of its token j, at position t = seq_lens[r] + j, is
  * slots[q_indptr[r] + j] = block_table[r][t / 16] * 16 + t % 16 (-1 where the
  * id is not in [0, 2^27)).  A request not granted keeps its counters, with
- * granted[r] = 0 and slots of -1.  new_free_count[0] = what is left.
+ * granted[r] = 0 and slots of -1.  Rows that are no request's, ahead of
+ * q_indptr[0] or from q_indptr[bs] on, have slots of -1.  new_free_count[0] =
+ * what is left.
  *
  * nsd_trim_blocks: request r keeps ceil(keep_lens[r] / 16) blocks (at most
  * owned[r]); the ids of its other blocks are pushed onto the free list,

@@ -154,9 +154,9 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PlanArgs A, int counters
     const int r = find(indptr, n, i);
     int32_t slot = -1;
     const int64_t t = (int64_t)lens[r] + (i - indptr[r]), b = t / NSD_BLOCK_SIZE;
-    // a granted request's tokens lie within its row (rows behind the last request's, and offsets
-    // that are no prefix sum, need not)
-    if (owned[r] >= 0 && t >= 0 && b < A.width && i < indptr[r + 1]) {
+    // a granted request's tokens lie within its row (rows ahead of the first request's or behind
+    // the last one's are no request's, and with offsets that are no prefix sum need not)
+    if (owned[r] >= 0 && t >= 0 && b < A.width && i >= indptr[r] && i < indptr[r + 1]) {
       const int64_t k = start[r] + (b - owned[r]);
       const int id = b < owned[r] ? A.table[(int64_t)r * A.width + b]
                      : k < free_n ? A.free_ids[free_n - 1 - k] : -1;

@@ -1,0 +1,27 @@
+"""Block plans at the edges of what their call allows, against the oracle."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_29364_amd as nsd
+from oracle import prompt
+from parity import i32
+from test_gpu_block_plan import make
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("ahead", [1, 5, 40, 5000])
+def test_rows_ahead_of_the_first_request_have_no_slot(device, ahead):
+    """Offsets that do not begin at 0: the rows before them are no request's, and a slot of theirs
+    would be one of the first request's cached tokens."""
+    table, owned, lens, indptr, free, count = make(8, 30, 20, 9, 60, lens_hi=100)
+    lens[0], owned[0] = 100, 20
+    table[0] = np.arange(500, 520)
+    indptr = indptr + ahead
+    rt, ro, rl, rc, rg, rs = prompt.plan_blocks(table, owned, lens, indptr, free, count, indptr[-1])
+    assert (rs[:ahead] == -1).all() and (rs[ahead:] >= 0).any()
+    t, o, l, q, f, c = (i32(x, device) for x in (table, owned, lens, indptr, free, [count]))
+    no, nl, nc, g, s = nsd.plan_blocks(t, o, l, q, f, c, int(indptr[-1]))
+    for a, b in ((t, rt), (no, ro), (nl, rl), (nc, [rc]), (g, rg), (s, rs)):
+        assert np.array_equal(a.cpu().numpy(), np.asarray(b))
