@@ -553,7 +553,8 @@ nsd_status nsd_sample_steps(const float* probs, int64_t row_stride, const float*
  * new_lens and new_free_count may be owned, seq_lens and free_count themselves
  * (updated in place); no other two arrays overlap.  Negative lengths and counts
  * count as 0, owned is clamped to the row, q_indptr to [0, total_q].
- * 0 <= bs <= 8192; free_capacity <= 2^27.  bs == 0 copies the count.
+ * 0 <= bs <= 8192; free_capacity <= 2^27.  bs == 0 copies the count, and every
+ * row's slot is -1.
  */
 nsd_status nsd_plan_blocks(int32_t* block_table, int32_t max_blocks_per_seq,
                            const int32_t* owned, const int32_t* seq_lens,

@@ -151,8 +151,12 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PlanArgs A, int counters
     A.table[(int64_t)r * A.width + owned[r] + (k - start[r])] = A.free_ids[free_n - 1 - k];
   }
   for (int i = at; i < A.total_q; i += step) {
-    const int r = find(indptr, n, i);
     int32_t slot = -1;
+    if (n == 0) {
+      A.slots[i] = slot;
+      continue;
+    }
+    const int r = find(indptr, n, i);
     const int64_t t = (int64_t)lens[r] + (i - indptr[r]), b = t / NSD_BLOCK_SIZE;
     // a granted request's tokens lie within its row (rows ahead of the first request's or behind
     // the last one's are no request's, and with offsets that are no prefix sum need not)
@@ -282,7 +286,7 @@ extern "C" nsd_status nsd_plan_blocks(int32_t* block_table, int32_t max_blocks_p
     return fail(NSD_ERR_NULL, "%s: NULL pointer argument", fn);
   const PlanArgs args{block_table, owned,     seq_lens,       q_indptr, free_blocks, free_count,
                       new_owned,   new_lens,  new_free_count, granted,  slots,       max_blocks_per_seq,
-                      free_capacity, bs, bs ? total_q : 0};
+                      free_capacity, bs, slots ? total_q : 0};
   const bool alias = new_owned == owned || new_lens == seq_lens || new_free_count == free_count;
   clear_stale_error();
   launch([](auto per) { return plan_kernel<decltype(per)::value>; }, args, args.total_q, alias, ((size_t)bs + 1) * 16, (hipStream_t)stream);

@@ -25,3 +25,13 @@ def test_rows_ahead_of_the_first_request_have_no_slot(device, ahead):
     no, nl, nc, g, s = nsd.plan_blocks(t, o, l, q, f, c, int(indptr[-1]))
     for a, b in ((t, rt), (no, ro), (nl, rl), (nc, [rc]), (g, rg), (s, rs)):
         assert np.array_equal(a.cpu().numpy(), np.asarray(b))
+
+
+@pytest.mark.parametrize("total", [1, 37, 9000])
+def test_rows_of_a_batch_of_none_have_no_slot(device, total):
+    e = torch.empty(0, dtype=torch.int32, device=device)
+    s = torch.full((total + 2,), 5, dtype=torch.int32, device=device)
+    out = nsd.plan_blocks(e.view(0, 4), e, e, i32([0], device), i32([1, 2, 3], device),
+                          i32([3], device), total, slots=s[1:-1])
+    assert out[2].item() == 3
+    assert (out[4] == -1).all() and s[0].item() == 5 and s[-1].item() == 5
