@@ -86,7 +86,7 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PlanArgs A, int counters
     len[i] = n ? A.lens[r] : 0;
     own[i] = n ? A.owned[r] : 0;
   }
-  int32_t need[PER];   // -1: more tokens than the table's row holds
+  int32_t need[PER];   // -1: more tokens than the table's row holds, or a length counts
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int r = i * kThreads + tid;
@@ -94,8 +94,9 @@ __global__ __launch_bounds__(kThreads) void plan_kernel(PlanArgs A, int counters
     count[i] = min(max(count[i], a[i]), A.total_q) - a[i];
     len[i] = max(len[i], 0);
     own[i] = min(max(own[i], 0), A.width);
-    const int64_t blocks = ((int64_t)len[i] + count[i] + NSD_BLOCK_SIZE - 1) / NSD_BLOCK_SIZE;
-    need[i] = blocks > A.width ? -1 : max((int32_t)blocks - own[i], 0);
+    const int64_t tokens = (int64_t)len[i] + count[i];
+    const int64_t blocks = (tokens + NSD_BLOCK_SIZE - 1) / NSD_BLOCK_SIZE;
+    need[i] = blocks > A.width || tokens > INT32_MAX ? -1 : max((int32_t)blocks - own[i], 0);
     if (r < n) {
       indptr[r] = a[i];
       lens[r] = len[i];

@@ -35,3 +35,16 @@ def test_rows_of_a_batch_of_none_have_no_slot(device, total):
                           i32([3], device), total, slots=s[1:-1])
     assert out[2].item() == 3
     assert (out[4] == -1).all() and s[0].item() == 5 and s[-1].item() == 5
+
+
+def test_lengths_past_31_bits_are_not_granted(device):
+    """A table row with room for more tokens than a length counts."""
+    width = 2**27 + 8
+    table = torch.zeros((1, width), dtype=torch.int32, device=device)
+    for length, n, ok in ((2**31 - 20, 19, 1), (2**31 - 20, 20, 0), (2**31 - 1, 100, 0)):
+        no, nl, nc, g, s = nsd.plan_blocks(table, i32([width], device), i32([length], device),
+                                           i32([0, n], device), i32([1, 2, 3], device),
+                                           i32([3], device), n)
+        assert g.item() == ok and nl.item() == length + n * ok and nc.item() == 3
+        assert no.item() == width
+        assert ((s >= 0) if ok else (s == -1)).all()
