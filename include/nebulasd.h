@@ -600,7 +600,9 @@ nsd_status nsd_trim_blocks(const int32_t* block_table, int32_t max_blocks_per_se
  * rot_dim : a multiple of 16 in [0, head_dim] (0: the rows are only cached).
  * slots : device int32 [total_q], as nsd_plan_blocks gives them.
  * k_pool, v_pool : this layer's planes; num_blocks <= 2^27.
- * head_dim in {64, 128}; block_size == 16.  total_q == 0 is a no-op.
+ * head_dim in {64, 128}; block_size == 16.  total_q == 0 is a no-op.  Rows and
+ * heads of 2^24 workgroups or more (2^26 rows of up to 32 heads are fewer) are
+ * refused.
  */
 nsd_status nsd_rope_append(void* k_pool, void* v_pool, int64_t num_blocks, const void* q,
                            int64_t q_stride, const void* k_new, int64_t k_stride,
@@ -646,7 +648,8 @@ nsd_status nsd_rope_append(void* k_pool, void* v_pool, int64_t num_blocks, const
  * workspace : device, 16-byte aligned, at least
  *     nsd_chunk_attention_workspace_size(...) bytes (may be 0), any contents;
  *     calls that overlap in time need separate ones.
- * 0 <= bs <= 8192; bs == 0 or total_q == 0 is a no-op.
+ * 0 <= bs <= 8192; bs == 0 or total_q == 0 is a no-op.  Batches of 2^24 items
+ * (128 rows of a KV head, and one more per request and KV head) are refused.
  */
 size_t     nsd_chunk_attention_workspace_size(int32_t bs, int32_t total_q, int32_t num_q_heads,
                                               int32_t num_kv_heads, int32_t head_dim,

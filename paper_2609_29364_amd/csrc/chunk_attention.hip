@@ -1091,7 +1091,8 @@ extern "C" nsd_status nsd_chunk_attention(
     return fail(NSD_ERR_WORKSPACE, "%s: a 16-byte aligned workspace of %zu bytes needed, %zu given",
                 fn, need, workspace ? workspace_size : (size_t)0);
   const int64_t groups = pieces(pl, num_kv_heads) * num_kv_heads;
-  if (groups > INT32_MAX) return fail(NSD_ERR_UNSUPPORTED, "%s: too many workgroups", fn);
+  if (groups * kThreads > UINT32_MAX)   // a launch's threads
+    return fail(NSD_ERR_UNSUPPORTED, "%s: too many workgroups", fn);
   Params P;
   P.q = (const uint16_t*)q;
   P.k = (const uint16_t*)k_cache;

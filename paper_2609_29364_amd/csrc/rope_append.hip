@@ -395,7 +395,8 @@ extern "C" nsd_status nsd_rope_append(void* k_pool, void* v_pool, int64_t num_bl
   A.query = kind(num_q_heads, 32);
   A.key = kind(num_kv_heads, 32);
   A.value = kind(num_kv_heads, 32);
-  if (blocks > INT32_MAX) return fail(NSD_ERR_UNSUPPORTED, "%s: too many workgroups", fn);
+  if (blocks * kThreads > UINT32_MAX)   // a launch's threads
+    return fail(NSD_ERR_UNSUPPORTED, "%s: too many workgroups", fn);
   const dim3 grid((uint32_t)blocks);
   clear_stale_error();
   auto go = [&](auto kernel) {
