@@ -647,13 +647,17 @@ nsd_status nsd_rope_append(void* k_pool, void* v_pool, int64_t num_blocks, const
  * q, out and the caches 16-byte aligned; out may not alias an input.
  * workspace : device, 16-byte aligned, at least
  *     nsd_chunk_attention_workspace_size(...) bytes (may be 0), any contents;
- *     calls that overlap in time need separate ones.
+ *     calls that overlap in time need separate ones.  A smaller batch can need
+ *     more than a larger one (the larger fills the device without being split);
+ *     nsd_chunk_attention_workspace_bound(...) bytes serve every batch of these
+ *     heads.
  * 0 <= bs <= 8192; bs == 0 or total_q == 0 is a no-op.  Batches of 2^24 items
  * (128 rows of a KV head, and one more per request and KV head) are refused.
  */
 size_t     nsd_chunk_attention_workspace_size(int32_t bs, int32_t total_q, int32_t num_q_heads,
                                               int32_t num_kv_heads, int32_t head_dim,
                                               int32_t max_q_per_seq, int32_t max_seq_len);
+size_t     nsd_chunk_attention_workspace_bound(int32_t num_kv_heads, int32_t head_dim);
 nsd_status nsd_chunk_attention(const void* q, const void* k_cache, const void* v_cache,
                                int64_t num_blocks, const int32_t* block_table,
                                int32_t max_blocks_per_seq, const int32_t* seq_lens,

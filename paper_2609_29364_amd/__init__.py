@@ -75,6 +75,7 @@ _SIGS = {
     "nsd_rope_append": (_I32, [_P, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P, _P, _P, _I32, _I32,
                                _I32, _P, _I32, _I32, _I32, _I32, _I32, _P, _P]),
     "nsd_chunk_attention_workspace_size": (_SZ, [_I32] * 7),
+    "nsd_chunk_attention_workspace_bound": (_SZ, [_I32] * 2),
     "nsd_chunk_attention": (_I32, [_P, _P, _P, _I64, _P, _I32, _P, _P, _I32, _I32, _I32, _I32, _I32,
                                    _I32, _I32, _I32, _F32, _F32, _P, _P, _P, _P, _P, _SZ, _P]),
     "nsd_check_plan": (_I32, [_P, _P, _I32, _P, _P, _I32, _I64, _I64, _I32, _I32, _I64]),
@@ -768,6 +769,12 @@ def chunk_attention_workspace_size(bs, total_q, num_q_heads, num_kv_heads, head_
                                                         head_dim, max_q_per_seq, max_seq_len))
 
 
+def chunk_attention_workspace_bound(num_kv_heads, head_dim):
+    """Bytes that serve chunk_attention for every batch of these heads (a smaller batch can need
+    more than a larger one)."""
+    return int(lib().nsd_chunk_attention_workspace_bound(num_kv_heads, head_dim))
+
+
 def chunk_attention(q, k_cache, v_cache, block_table, seq_lens, q_indptr, max_q_per_seq,
                     max_seq_len, scale=None, softcap=0.0, slopes=None, first_keys=None,
                     prefix_lens=None, out=None, workspace=None):
@@ -779,7 +786,8 @@ def chunk_attention(q, k_cache, v_cache, block_table, seq_lens, q_indptr, max_q_
     score times the distance of query and key; first_keys: int32 [total_q], the first token each
     query sees (a sliding window, a packed document); prefix_lens: int32 [bs], leading tokens
     every query of the request sees.  workspace: chunk_attention_workspace_size(bs, total_q, ...)
-    bytes (allocated per call when None)."""
+    bytes, or chunk_attention_workspace_bound(...) for batches of any size (allocated per call when
+    None)."""
     r = (_native_module or _native()).chunk_attention(
         q, k_cache, v_cache, block_table, seq_lens, q_indptr, max_q_per_seq, max_seq_len, scale,
         softcap, slopes, first_keys, prefix_lens, out, workspace)
@@ -836,4 +844,5 @@ __all__ = ["lib", "version", "attention_waves", "check_plan", "check_pairs", "kv
            "new_workspace", "gather_verify_attention", "copy_plan", "COPY_H2D", "COPY_D2H",
            "DEFAULT_CHUNK", "kv_append", "commit_lengths", "host_alias", "kv_writeback",
            "spec_accept", "spec_accept_static", "accept_workspace_size", "sample", "plan_blocks",
-           "trim_blocks", "rope_append", "chunk_attention", "chunk_attention_workspace_size", "NsdError", "BLOCK_SIZE", "LIB_PATH"]
+           "trim_blocks", "rope_append", "chunk_attention", "chunk_attention_workspace_size",
+           "chunk_attention_workspace_bound", "NsdError", "BLOCK_SIZE", "LIB_PATH"]

@@ -1050,6 +1050,11 @@ extern "C" size_t nsd_chunk_attention_workspace_size(int32_t bs, int32_t total_q
                          head_dim);
 }
 
+extern "C" size_t nsd_chunk_attention_workspace_bound(int32_t num_kv_heads, int32_t head_dim) {
+  if (num_kv_heads < 1 || (head_dim != 64 && head_dim != 128)) return 0;
+  return workspace_bound(num_kv_heads, head_dim);
+}
+
 extern "C" nsd_status nsd_chunk_attention(
     const void* q, const void* k_cache, const void* v_cache, int64_t num_blocks,
     const int32_t* block_table, int32_t max_blocks_per_seq, const int32_t* seq_lens,

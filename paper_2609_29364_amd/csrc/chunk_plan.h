@@ -49,6 +49,9 @@ constexpr Tail last_round(int items, int hkv) {
   return Tail{over, std::min(round / over, 16)};
 }
 
+// The most parts of a batch, per KV head (see plan()).
+int64_t most_places(int32_t hkv) { return 2 * kSlots / hkv + 1; }
+
 // Bounds per KV head: a batch's items, the split ones of them and their parts.
 struct Plan {
   int tile;        // rows of an item
@@ -76,9 +79,8 @@ Plan plan(int32_t bs, int32_t total_q, int32_t hq, int32_t hkv, int32_t max_len)
   // A tile of s stages has at most 1 + s / limit <= 2 s / limit parts if it is split, and the
   // tiles' s sum to the total: at most 2 total / limit places, where limit is at least the
   // share total / (kSlots / hkv); also at most kMaxSplits and ceil(stages / 4) a tile.
-  const int64_t share = 2 * kSlots / hkv + 1;
   const int64_t each = std::min<int64_t>(kMaxSplits, (stages + 3) / 4);
-  p.places = (int)std::min(share, p.items * each);
+  p.places = (int)std::min(most_places(hkv), p.items * each);
   p.split_items = (int)std::min<int64_t>(p.places / 2, p.items);
   if (p.split_items == 0) p.places = 0;   // (more KV heads than workgroups to split for)
   return p;
@@ -88,6 +90,16 @@ size_t workspace_bytes(const Plan& p, int32_t hkv, int32_t d) {
   // the count, the records, then (max, sum) and rows of every place
   return p.places ? 16 + (size_t)p.split_items * hkv * 16 +
                         (size_t)p.places * hkv * kRows * (8 + (size_t)d * 4) : 0;
+}
+
+// What workspace_bytes() is at most for any batch of these heads.  (It does not rise with the batch:
+// one token after 4096 is split for every slot of the device, 256 of them are not.)
+size_t workspace_bound(int32_t hkv, int32_t d) {
+  Plan p{};
+  p.places = (int)most_places(hkv);
+  p.split_items = p.places / 2;
+  if (p.split_items == 0) p.places = 0;
+  return workspace_bytes(p, hkv, d);
 }
 
 // Workgroups per KV head: the items, and parts beyond the first of each, which are fewer than

@@ -126,3 +126,13 @@ def test_one_long_context_among_many_items(device):
     pos = np.concatenate([np.arange(c, c + n) for c, n in zip(b.ctx, b.new)])
     kw = dict(first=np.maximum(pos - 8000, 0), prefix=[20] * bs, softcap=30.0)
     b.check(b.run(**kw), **kw)
+
+
+def test_one_workspace_for_batches_of_any_size(device):
+    ws = nsd.new_workspace(nsd.chunk_attention_workspace_bound(8, 64), device)
+    rng = np.random.default_rng(2)
+    for bs, hi in ((256, 300), (100, 900), (7, 2000), (1, 4000), (30, 1200)):
+        new = np.ones(bs, int)
+        new[0] = 20
+        b = Batch(device, rng.integers(0, hi, bs).tolist(), new.tolist(), 16, 8, 64, seed=bs)
+        b.check([b.run(bound=4096, workspace=ws), b.run(bound=100000, workspace=ws)])
