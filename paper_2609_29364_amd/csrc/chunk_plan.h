@@ -38,7 +38,7 @@ constexpr int parts_of(int stages, float limit) {
 }
 
 // Where none is split so, the items that would begin a last round less than half full are split
-// to fill it: two ragged chunks (194 tiles a head) 2897 -> 2530 us, 8300 tokens after 24000 3712
+// to fill it: two ragged chunks (193 items a head) 2897 -> 2530 us, 8300 tokens after 24000 3712
 // -> 3400.
 struct Tail {
   int items, parts;
@@ -71,11 +71,16 @@ Plan plan(int32_t bs, int32_t total_q, int32_t hq, int32_t hkv, int32_t max_len)
          ((int64_t)total_q * (hq / hkv) / (p.tile / 2) + bs) * hkv <= kSlots)
     p.tile /= 2;
   p.items = (int64_t)total_q * (hq / hkv) / p.tile + bs;
-  // The second launch does not pay for itself where the items make two rounds or more of
-  // contexts to 8192 tokens (packed documents, 4 requests to 6000 tokens: 105 us without, 122
-  // with it), nor where all are short; one much longer item among many does.
+  // Where the items make two rounds or more, parts, their order and the second launch win only if
+  // one context is much longer than the rest (us without -> with them, the longest context 4000
+  // / 8000 tokens: one single token after it among 200 after 64 48 -> 50 / 86 -> 50, one of 256
+  // chunks of 100 tokens 51 -> 32 / 94 -> 32).  Single tokens after a quarter of it to all of it
+  // lose 324 -> 331 / 633 -> 636, in windows of 512 86 -> 94 / 84 -> 92; prompts of like lengths 509
+  // -> 517 / 1887 -> 1904, ragged ones 541 -> 555 / 1308 -> 1335, of packed documents 206 -> 219 /
+  // 367 -> 407.  The host knows the longest context alone: the lone one counts beyond 8192 tokens.
+  // Where all contexts are short nothing is split.
   p.split_items = p.places = 0;
-  if (bs > kPartedBatch || stages <= (p.items * hkv > 2 * kSlots ? 129 : 12)) return p;
+  if (bs > kPartedBatch || stages <= (p.items * hkv > 2 * kSlots ? 8192 / kStage : 12)) return p;
   // A tile of s stages has at most 1 + s / limit <= 2 s / limit parts if it is split, and the
   // tiles' s sum to the total: at most 2 total / limit places, where limit is at least the
   // share total / (kSlots / hkv); also at most kMaxSplits and ceil(stages / 4) a tile.

@@ -140,3 +140,12 @@ def test_room_for_parts_has_room_for_their_records(count, hkv, max_len):
         c = count([0] * bs + [total], [max_len] * bs, total, hkv, hkv, max_len)
         assert (c["room"] == 0) == (c["records"] == 0), (bs, total)
         assert c["records"] * 2 <= c["room"] and sound(c)
+
+
+def test_lines(count):
+    """Batches of more than two rounds are split beyond 8192 tokens, smaller ones beyond 768, and
+    of more than 256 requests none."""
+    room = lambda bs, max_len, hkv=8: count(range(bs + 1), [1] * bs, bs, 4 * hkv, hkv, max_len)["room"]
+    assert room(125, 768) == 0 < room(125, 769) and room(125, 8192) > 0
+    assert room(126, 8192) == 0 < room(126, 8193)
+    assert room(256, 8193) > 0 == room(257, 2**31 - 1, 1)
