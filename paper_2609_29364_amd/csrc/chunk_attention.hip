@@ -21,20 +21,21 @@
 // (rounded to bf16, an error of at most 2^-8 of each weight) without leaving
 // its lane.
 //
-// The softmax rescale is skipped while no row's maximum grows by more than 2^8
-// (weights then stay below 2^8, far from any limit of fp32).  Tokens hidden
-// from a row get weight 0; as 0 times an infinity or NaN is NaN, a V operand of
-// a stage with hidden tokens is looked through for them, and where one has any
-// they are taken out of the product and added to the rows that see them.
+// The softmax rescale is skipped while no row's maximum grows by more than 8 in log2
+// (weights then stay below 2^8, far from any limit of fp32), a published refinement of the one-pass
+// softmax.  Tokens hidden from a row get weight 0; as 0 times an infinity or NaN is NaN, a V operand
+// of a stage with hidden tokens is looked through for them, and where one has any they are taken out
+// of the product and added to the rows that see them.
 //
 // Items of at most 64 rows (single tokens, ends of chunks) are bound by memory: their
 // waves stream K and V into registers, each its own tokens.  Larger ones are bound by the
 // matrix cores and, about as much, the ALU that runs the softmax.  Measured (32/8 heads,
-// head_dim 128): 8192 tokens after 24000 3242 us, 1163 TFLOP/s, the matrix cores busy 63 % of
-// the cycles (the card's library product reaches 1120-1580 TFLOP/s by size); four prompts of
-// 4096 tokens 530 us, 1038 TFLOP/s; 256 single tokens at 1-4k 416 us, 6.5 TB/s; 128 of them at
-// 2-8k, capped, in a window of 1024 behind a prefix 100 us, 5.7 TB/s.  128 rows rather than 256:
-// two workgroups of four waves on a CU rather than one of eight, which all wait at one barrier.
+// head_dim 128): 8192 tokens after 24000 3240-3340 us, 1130-1163 TFLOP/s, the matrix cores busy
+// 63 % of the cycles (the card's library product reaches 1120-1580 TFLOP/s by size); four prompts
+// of 4096 tokens 530-546 us, 1007-1038 TFLOP/s; 256 single tokens at 1-4k 412-416 us, 6.5 TB/s; 128
+// of them at 2-8k, capped, in a window of 1024 behind a prefix 97-99 us, 5.8 TB/s.  128 rows rather
+// than 256: two workgroups of four waves on a CU rather than one of eight, which all wait at one
+// barrier.
 #include "chunk_plan.h"
 #include "nsd_internal.h"
 
@@ -387,6 +388,7 @@ __device__ inline bf16x8 ones(uint32_t m) {
 // 2^-22 of the cap or so whatever the score, which up to kUsual is 2^-14 of a weight, a 64th of
 // its rounding to bf16.  kLargeCap, for caps beyond: the series of tanh where |x / cap| < 1/4 (its
 // next term is 2^-26 of the score there), so that the error is about 5 2^-23 of the score itself.
+// It costs prompts of packed documents 106 -> 141 us, single tokens 97 -> 98.
 template <int CAP, bool BIAS, int NSUB>
 __device__ inline void to_log2(f32x16 (&s)[NSUB], float c, float cap, const Sight& w, int t0,
                                int half) {

@@ -692,7 +692,6 @@ PyObject* py_draft_stage(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// bind(addresses): the library's entry points, in the order of Api.
 // The prompt path's tensors lie on the current device, all of them (the Python path switches
 // to another device, or names the tensor that is elsewhere).
 at::Device here(const Tensor& t) {
@@ -899,6 +898,7 @@ PyObject* py_chunk_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// bind(addresses): the library's entry points, in the order of Api.
 PyObject* py_bind(PyObject*, PyObject* addresses) {
   void** to = (void**)&api;
   const Py_ssize_t n = sizeof(Api) / sizeof(void*);
