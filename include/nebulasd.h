@@ -527,8 +527,8 @@ nsd_status nsd_sample_steps(const float* probs, int64_t row_stride, const float*
  * served in order: r is granted if it needs none, or if its needs and those of
  * all requests before it (granted or not) are at most free_count[0].  A request
  * whose tokens do not fit its table row (ceil(..) > max_blocks_per_seq), or are
- * more than 2^31 - 1, is not granted and counts no need.  The free list is a stack, free_blocks[0 ..
- * free_count[0]), whose last entry is taken first.
+ * more than 2^31 - 1, is not granted and counts no need.  The free list is a
+ * stack, free_blocks[0 .. free_count[0]), whose last entry is taken first.
  *
  * nsd_plan_blocks: a granted request's new ids go to its table row's entries
  * owned[r].. (no other entry is written); granted[r] = 1,
